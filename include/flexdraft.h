@@ -11,13 +11,16 @@
  *   fd_accept_greedy       lossless acceptance, temperature -> 0 (Sec. 3)
  *   fd_accept_sample       lossless acceptance by speculative sampling (Sec. 3)
  *
+ * and, around them, the commit of accepted rows, the choice of drafts, the tables of a step,
+ * the norm and rotation of queries and keys, and the same attention over a cache held in 4 bits.
+ *
  * General conventions
  *   - Plain C.  Every pointer marked "device" is a HIP device pointer on the
  *     current device; pointers marked "host" are ordinary host memory.
  *   - The caller owns every buffer.  The library never allocates or frees device
  *     memory and never synchronises the stream.  The KV cache is read-only to every
  *     call except fd_append_kv, which receives it through separate, writable
- *     pointers.
+ *     pointers, and fd_append_kv_q4.
  *   - All work is enqueued on `hip_stream` (a hipStream_t passed as void*; NULL
  *     is the default stream) and the call returns immediately.
  *   - The return value is the only host-side error channel.  Argument errors are
@@ -313,6 +316,149 @@ FD_API fd_status fd_select_branch(const int32_t *block_tokens, const int32_t *bl
                                   int32_t batch, int32_t total_tokens,
                                   int32_t out_stride, int32_t *out_tokens, int32_t *out_block,
                                   void *hip_stream);
+
+/*
+ * ---- Around the attention call: tables of a step, norm and rotation, a cache held in 4 bits ----
+ */
+
+/*
+ * Arguments of fd_step_tables: the tables of a decoding step from the requests' lengths, which only the device
+ * knows once fd_append_kv has moved kv_len and fd_draft_select has said how many drafts are worth verifying.
+ *
+ * Request i brings n_i = k_i + m_i new rows, k_i = verify_len[i] verify rows and m_i = mask_rows[i] mask rows, and
+ * needs need_i = ceil((kv_len[i] + k_i) / page_size) pages: its cached tokens and every row that may be
+ * committed.  It holds the first table_len[i] entries of its row of block_table.
+ *   1. Requests that hold more give back entries need_i .. table_len[i) of their row: they are appended to
+ *      free_pages (a stack of free_count[0] entries), request by request, in the order of the row.  A request that has ended
+ *      (kv_len 0, no rows) gives back all it holds.
+ *   2. Requests that hold fewer take pages off the top of that stack, request by request, one entry after the other.
+ *      A stack that runs out leaves the requests that come later short (FD_DEV_PAGE_RANGE; page lists then end early).
+ *   3. row_indptr, page_indptr and page_indices are what fd_attn_args wants: prefix sums of n_i and of the
+ *      pages listed, and the lists.  Row r of request i gets
+ *        positions[row]  kv_len[i] + r for a verify row; kv_len[i] + v_ib + j for row j of mask block b, which continues the
+ *                        v_ib verify rows that block sees (mask_vis, mask_blocks and their defaults as in fd_attn_args)
+ *        slot_map[row]   page * page_size + slot of that position for a verify row, -1 for a mask row
+ * The call reads table_len and free_count and writes table_len_out and free_count_out, which may be the same arrays.
+ */
+typedef struct fd_table_args {
+  int32_t batch;              /* B in [0, 65535]                                              */
+  int32_t page_size;          /* tokens per page, >= 1                                        */
+  int32_t table_stride;       /* entries per row of block_table, <= 2^20                      */
+  int32_t total_rows;         /* entries of positions and slot_map, <= 2^20: rows past them are dropped (FD_DEV_ROWS_RANGE) */
+  int32_t page_indices_len;   /* entries of page_indices: lists end there (FD_DEV_PAGE_RANGE) */
+  int32_t free_pages_len;     /* entries of free_pages: pages given back past them are lost (FD_DEV_PAGE_RANGE) */
+  const int32_t *kv_len;      /* device [B]                                                   */
+  const int32_t *verify_len;  /* device [B]                                                   */
+  const int32_t *mask_rows;   /* device [B] or NULL (=> 0)                                    */
+  const int32_t *mask_vis;    /* device [B] or NULL, as in fd_attn_args                       */
+  const int32_t *mask_blocks; /* device [B] or NULL, as in fd_attn_args                       */
+  int32_t *block_table;       /* device [B][table_stride], updated                            */
+  const int32_t *table_len;   /* device [B]                                                   */
+  int32_t *table_len_out;     /* device [B]; may be table_len                                 */
+  int32_t *free_pages;        /* device [free_pages_len], updated                             */
+  const int32_t *free_count;  /* device [1]                                                   */
+  int32_t *free_count_out;    /* device [1]; may be free_count                                */
+  int32_t *row_indptr;        /* device [B+1]                                                 */
+  int32_t *page_indptr;       /* device [B+1]                                                 */
+  int32_t *page_indices;      /* device [page_indices_len]                                    */
+  int32_t *positions;         /* device [total_rows] or NULL                                  */
+  int64_t *slot_map;          /* device [total_rows] or NULL                                  */
+  uint32_t *status;           /* device uint32[1] or NULL; caller zeroes it                   */
+} fd_table_args;
+
+/* Asynchronous on hip_stream.  Lengths out of range (negative, kv_len above 2^30, more pages than table_stride) are
+ * clamped and reported through status.  Errors: FD_ERR_INVALID_ARG, FD_ERR_UNSUPPORTED, FD_ERR_HIP. */
+FD_API fd_status fd_step_tables(const fd_table_args *args, void *hip_stream);
+
+/*
+ * Arguments of fd_qk_norm_rope: root-mean-square norm of every query and key head and their rotation by position,
+ * the pass between the projections and fd_verify_draft_attn.  For a head x of D = head_dim elements
+ *     y = x / sqrt(mean(x^2) + eps) * weight               (y = x where the weight is NULL)
+ *     (y_a, y_b) -> (y_a cos t - y_b sin t, y_b cos t + y_a sin t),  t = positions[row] * inv_freq[i]
+ * for the pairs i < rotary_dim / 2: a = i, b = i + rotary_dim / 2, or with interleaved != 0 a = 2 i, b = 2 i + 1; elements from
+ * rotary_dim on are not rotated.  Everything is computed in fp32 (the angle's turns in fp64) and rounded once.
+ * Inputs are [total_rows][heads][D] with strides in elements between rows and heads (multiples of 4; the last dimension is
+ * contiguous), so the parts of one fused projection can be given as they are.  Outputs are dense.  q_out may be q and
+ * k_out may be k where the input is dense; else no output may overlap an input.  v and v_out, if given, are
+ * num_kv_heads heads that are copied as they are.
+ */
+typedef struct fd_rope_args {
+  int32_t total_rows;         /* R >= 0                                                       */
+  int32_t num_q_heads;        /* >= 0                                                         */
+  int32_t num_kv_heads;       /* >= 0                                                         */
+  int32_t head_dim;           /* D: multiple of 8, <= 256                                     */
+  int32_t rotary_dim;         /* multiple of 8 in [0, D]                                      */
+  int32_t interleaved;        /* pairs side by side instead of half a rotary_dim apart        */
+  int32_t dtype;              /* fd_dtype of q, k, v, the weights and the outputs             */
+  float   eps;                /* >= 0                                                         */
+  const void *q, *k, *v;      /* device; v may be NULL                                        */
+  int64_t q_stride_row, q_stride_head, k_stride_row, k_stride_head, v_stride_row, v_stride_head;
+  void *q_out, *k_out, *v_out;/* device, dense; v_out is NULL exactly when v is               */
+  const void *q_weight;       /* device [D] or NULL: no norm                                  */
+  const void *k_weight;       /* device [D] or NULL: no norm                                  */
+  const float *inv_freq;      /* device [rotary_dim / 2]; may be NULL with rotary_dim 0       */
+  const int32_t *positions;   /* device [R]; may be NULL with rotary_dim 0                    */
+} fd_rope_args;
+
+/* Asynchronous on hip_stream.  Errors: FD_ERR_INVALID_ARG, FD_ERR_UNSUPPORTED, FD_ERR_HIP. */
+FD_API fd_status fd_qk_norm_rope(const fd_rope_args *args, void *hip_stream);
+
+/*
+ * A paged KV cache held in 4 bits.  A code is a sign (bit 3) and a magnitude 0, 1/2, 1, 3/2, 2, 3, 4, 6 (bits 2..0);
+ * rounding is to nearest, ties to the even code.
+ *   keys    32 channels of a token and head share a power of two 2^e: the smallest with |k| <= 6 * 2^e (e >= -126).
+ *           k_codes   [page][head][slot][D/2] bytes, the even channel in the low half
+ *           k_scales  [page][head][slot][D/32] bytes, e + 127
+ *   values  a token and head have one scale, bf16(max |v| / 6).
+ *           v_codes   [page][head][slot/16][8 D] bytes: for sixteen slots [slot/8 % 2][j < 32][c < D/32] four bytes that hold channel
+ *                     32 c + j of eight slots, the even slot in the low half: the layout in which the attention kernel's
+ *                     lanes take them, sixteen bytes each
+ *           v_scales  [page][head][slot] bf16
+ * 134 bytes a token and head at D = 128, where bf16 takes 512.  A group of keys, or a token's values, that holds an infinity or
+ * a NaN is stored as NaN.  D is 128 or 64, page_size a multiple of 16.  The block (page p, head g) of each array is number
+ * p * stride_page + g * stride_head (dense: num_kv_heads and 1).
+ */
+typedef struct fd_q4_cache {
+  void *k_codes;              /* device, 16-byte aligned                                      */
+  void *k_scales;             /* device, 4-byte aligned                                       */
+  void *v_codes;              /* device, 16-byte aligned                                      */
+  void *v_scales;             /* device, 16-byte aligned                                      */
+  int64_t stride_page, stride_head;   /* in blocks                                            */
+} fd_q4_cache;
+
+/*
+ * fd_verify_draft_attn over a cache in 4 bits: the same operation, rows, masks, page lists, outputs and status bits.
+ * args->k_cache, v_cache and the cache strides are not used; dtype (of q, k_new, v_new and out) is FD_BF16, head_dim 128 or 64,
+ * page_size a multiple of 16.  The step's own rows take part in bf16, as they are.  FD_ATTN_PLANNED is
+ * ignored (there is nothing to plan), FD_ATTN_FORCE_GENERIC refused.  kv_chunk > 0 (a multiple of 64) is the number of keys
+ * of one sequence and head that a work-group takes.  Workspace: fd_verify_draft_attn_q4_workspace(args) bytes, device,
+ * 256-byte aligned; nothing in it has to start at zero or survive a call, and calls that may overlap need one each.
+ * Asynchronous on hip_stream.  Errors: FD_ERR_INVALID_ARG, FD_ERR_UNSUPPORTED, FD_ERR_WORKSPACE_TOO_SMALL, FD_ERR_HIP.
+ */
+FD_API fd_status fd_verify_draft_attn_q4(const fd_attn_args *args, const fd_q4_cache *cache, void *hip_stream);
+FD_API size_t fd_verify_draft_attn_q4_workspace(const fd_attn_args *args);
+
+/*
+ * fd_append_kv into a cache in 4 bits: new rows 0 .. accept_len[i] of every sequence are rounded and written (a prompt is a
+ * sequence whose rows are all accepted).  Fields of args read, checks and kv_len_out as in fd_append_kv; dtype is FD_BF16.
+ * Two slots share a byte of v_codes: a page that another sequence's list holds too must not be appended to.
+ */
+FD_API fd_status fd_append_kv_q4(const fd_attn_args *args, const fd_q4_cache *cache, const int32_t *accept_len,
+                                 int32_t *kv_len_out, void *hip_stream);
+
+/*
+ * What a cache in 4 bits stands for: tokens start[i] .. start[i] + out_indptr[i+1] - out_indptr[i] of sequence i become rows
+ * out_indptr[i] .. of k_out and v_out, [total_rows][num_kv_heads][head_dim] dense, FD_F32 (exactly the values) or FD_BF16
+ * (values rounded).  Tokens that the page list has no place for leave their rows as they were (FD_DEV_PAGE_RANGE).
+ *   start       device int32 [B] or NULL (=> 0)
+ *   out_indptr  device int32 [B+1]
+ *   status      device uint32[1] or NULL
+ * Asynchronous on hip_stream.  Errors: FD_ERR_INVALID_ARG, FD_ERR_UNSUPPORTED, FD_ERR_HIP.
+ */
+FD_API fd_status fd_read_kv_q4(const fd_q4_cache *cache, int32_t batch, int32_t num_kv_heads, int32_t head_dim, int32_t page_size,
+                               int32_t num_pages, const int32_t *page_indptr, const int32_t *page_indices, int32_t page_indices_len,
+                               const int32_t *start, const int32_t *out_indptr, int32_t total_rows, void *k_out, void *v_out,
+                               fd_dtype out_dtype, uint32_t *status, void *hip_stream);
 
 /* Thread-local description of the last error returned on this thread ("" if none). */
 FD_API const char *fd_last_error(void);

@@ -13,7 +13,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libflexdraft.so")
 PROBES_LIB = os.path.join(HERE, "libfdprobes.so")
-SOURCES = ["api.hip", "attn_generic.hip", "attn_mfma.hip", "accept.hip", "append.hip"]
+SOURCES = ["api.hip", "attn_generic.hip", "attn_mfma.hip", "accept.hip", "append.hip", "tables.hip", "rope.hip", "kv_q4.hip", "attn_q4.hip"]
 PROBE_SOURCES = ["probes.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-fvisibility=hidden",

@@ -1,6 +1,6 @@
 // C ABI of the library: argument validation, launch-shape decisions, workspace layout.
 // Every entry point is declared and documented in include/flexdraft.h.
-#include "fd_common.h"
+#include "kv_q4.h"
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
@@ -22,6 +22,14 @@ hipError_t run_append_kv(const AttnParams& p, int dtype, void* k_cache, void* v_
 hipError_t run_select_branch(const int* block_tokens, const int* block_indptr, const int* mask_blocks,
                              const int* accept_len, const int* first_vis, const int* verify_len, int batch,
                              int total_tokens, int out_stride, int* out_tokens, int* out_block, hipStream_t st);
+hipError_t run_step_tables(const fd_table_args& a, hipStream_t st);
+hipError_t run_qk_norm_rope(const fd_rope_args& a, hipStream_t st);
+size_t attn_q4_workspace(int batch, int num_kv_heads, int group, int total_rows, int max_kv_len, int max_new_rows, int kv_chunk, int head_dim);
+hipError_t run_attn_q4(const AttnParams& p, const Q4Cache& c, void* workspace, int kv_chunk, hipStream_t st);
+hipError_t run_append_kv_q4(const AttnParams& p, const Q4Cache& c, const int* accept_len, int* kv_len_out, hipStream_t st);
+hipError_t run_read_kv_q4(const Q4Cache& c, int batch, int num_kv_heads, int head_dim, int page_size, int num_pages, const int* page_indptr,
+                          const int* page_indices, int page_entries, const int* start, const int* out_indptr, int total_rows, void* k_out,
+                          void* v_out, int dtype, uint32_t* status, hipStream_t st);
 int attn_mfma_tile_keys();
 int attn_mfma_rows_per_wg(int max_tile_rows);
 hipError_t run_attn_mfma_plan(const AttnParams& p, void* workspace, int kv_chunk, hipStream_t st);
@@ -462,6 +470,187 @@ fd_status fd_select_branch(const int32_t* block_tokens, const int32_t* block_ind
                                        total_tokens, out_stride, out_tokens, out_block,
                                        reinterpret_cast<hipStream_t>(hip_stream));
   if (e != hipSuccess) return fail(FD_ERR_HIP, "select_branch launch: %s", hipGetErrorString(e));
+  return FD_OK;
+}
+
+// ---- tables, norm and rotation, the cache in 4 bits ---------------------------------------------
+
+fd_status fd_step_tables(const fd_table_args* a, void* hip_stream) {
+  if (!a) return fail(FD_ERR_INVALID_ARG, "args is NULL");
+  if (a->batch < 0 || a->table_stride < 0 || a->total_rows < 0 || a->page_indices_len < 0 || a->free_pages_len < 0)
+    return fail(FD_ERR_INVALID_ARG, "negative size (batch %d, table_stride %d, total_rows %d, page_indices_len %d, free_pages_len %d)", a->batch,
+                a->table_stride, a->total_rows, a->page_indices_len, a->free_pages_len);
+  if (a->page_size <= 0) return fail(FD_ERR_INVALID_ARG, "page_size %d must be positive", a->page_size);
+  if (a->batch > 65535) return fail(FD_ERR_UNSUPPORTED, "batch %d > 65535", a->batch);
+  if (a->table_stride > (1 << 20) || a->total_rows > (1 << 20)) return fail(FD_ERR_UNSUPPORTED, "table_stride %d / total_rows %d above 2^20", a->table_stride, a->total_rows);
+  if (a->page_indices_len > (1 << 30) || a->free_pages_len > (1 << 30)) return fail(FD_ERR_UNSUPPORTED, "page_indices_len / free_pages_len above 2^30");
+  if (!a->row_indptr || !a->page_indptr || !a->free_count || !a->free_count_out ||
+      (a->batch > 0 && (!a->kv_len || !a->verify_len || !a->table_len || !a->table_len_out)))
+    return fail(FD_ERR_INVALID_ARG, "a required device pointer is NULL");
+  if ((a->batch > 0 && a->table_stride > 0 && !a->block_table) || (a->page_indices_len > 0 && !a->page_indices) || (a->free_pages_len > 0 && !a->free_pages))
+    return fail(FD_ERR_INVALID_ARG, "block_table, page_indices or free_pages is NULL");
+  g_err[0] = 0;
+  hipError_t e = fd::run_step_tables(*a, reinterpret_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return fail(FD_ERR_HIP, "step tables launch: %s", hipGetErrorString(e));
+  return FD_OK;
+}
+
+fd_status fd_qk_norm_rope(const fd_rope_args* a, void* hip_stream) {
+  if (!a) return fail(FD_ERR_INVALID_ARG, "args is NULL");
+  if (a->total_rows < 0 || a->num_q_heads < 0 || a->num_kv_heads < 0)
+    return fail(FD_ERR_INVALID_ARG, "negative size (total_rows %d, num_q_heads %d, num_kv_heads %d)", a->total_rows, a->num_q_heads, a->num_kv_heads);
+  if (a->head_dim <= 0 || a->head_dim % 8) return fail(FD_ERR_INVALID_ARG, "head_dim %d must be a positive multiple of 8", a->head_dim);
+  if (a->head_dim > 256) return fail(FD_ERR_UNSUPPORTED, "head_dim %d > 256 has no kernel", a->head_dim);
+  if (a->rotary_dim < 0 || a->rotary_dim > a->head_dim || a->rotary_dim % 8)
+    return fail(FD_ERR_INVALID_ARG, "rotary_dim %d must be a multiple of 8 from 0 to head_dim %d", a->rotary_dim, a->head_dim);
+  if (a->dtype != FD_F32 && a->dtype != FD_BF16) return fail(FD_ERR_INVALID_ARG, "unknown dtype %d", a->dtype);
+  if (!(a->eps >= 0.f) || isinf(a->eps)) return fail(FD_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  if (a->num_q_heads > 4096 || a->num_kv_heads > 4096) return fail(FD_ERR_UNSUPPORTED, "%d / %d heads > 4096", a->num_q_heads, a->num_kv_heads);
+  g_err[0] = 0;
+  if (a->total_rows == 0 || a->num_q_heads + a->num_kv_heads == 0) return FD_OK;
+  if ((a->num_q_heads > 0 && (!a->q || !a->q_out)) || (a->num_kv_heads > 0 && (!a->k || !a->k_out)))
+    return fail(FD_ERR_INVALID_ARG, "a required device pointer is NULL");
+  if (a->num_kv_heads > 0 && !a->v != !a->v_out) return fail(FD_ERR_INVALID_ARG, "v and v_out are given together or not at all");
+  if (a->rotary_dim > 0 && (!a->inv_freq || !a->positions)) return fail(FD_ERR_INVALID_ARG, "rotary_dim > 0 needs inv_freq and positions");
+  const int64_t strides[] = {a->q_stride_row, a->q_stride_head, a->k_stride_row, a->k_stride_head, a->v ? a->v_stride_row : 0, a->v ? a->v_stride_head : 0};
+  for (int64_t s : strides)
+    if (s < 0 || s % 4) return fail(FD_ERR_INVALID_ARG, "strides must be non-negative multiples of 4 elements (%lld)", (long long)s);
+  const void* ptrs[] = {a->q, a->k, a->v, a->q_out, a->k_out, a->v_out, a->q_weight, a->k_weight};
+  for (const void* p : ptrs)
+    if (!aligned16(p)) return fail(FD_ERR_INVALID_ARG, "q, k, v, the weights and the outputs must be 16-byte aligned");
+  hipError_t e = fd::run_qk_norm_rope(*a, reinterpret_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return fail(FD_ERR_HIP, "norm and rotation launch: %s", hipGetErrorString(e));
+  return FD_OK;
+}
+
+static fd_status check_q4_cache(const fd_q4_cache* c, int head_dim, int page_size, int num_kv_heads) {
+  if (!c) return fail(FD_ERR_INVALID_ARG, "cache is NULL");
+  if (head_dim != 128 && head_dim != 64) return fail(FD_ERR_UNSUPPORTED, "a cache in 4 bits has head_dim 128 or 64, not %d", head_dim);
+  if (page_size <= 0 || page_size % 16) return fail(page_size <= 0 ? FD_ERR_INVALID_ARG : FD_ERR_UNSUPPORTED, "page_size %d of a cache in 4 bits must be a positive multiple of 16", page_size);
+  if (num_kv_heads <= 0 || num_kv_heads > 65535) return fail(FD_ERR_INVALID_ARG, "num_kv_heads %d", num_kv_heads);
+  if (c->stride_page < 0 || c->stride_head < 0 || c->stride_page >= (1ll << 31) || c->stride_head >= (1ll << 31))
+    return fail(FD_ERR_INVALID_ARG, "cache strides must be in [0, 2^31) blocks");
+  if (!aligned16(c->k_codes) || !aligned16(c->v_codes) || !aligned16(c->v_scales) || (reinterpret_cast<uintptr_t>(c->k_scales) & 3))
+    return fail(FD_ERR_INVALID_ARG, "k_codes, v_codes and v_scales must be 16-byte aligned, k_scales 4-byte aligned");
+  return FD_OK;
+}
+static bool q4_cache_complete(const fd_q4_cache* c) { return c->k_codes && c->k_scales && c->v_codes && c->v_scales; }
+static fd::Q4Cache q4_cache(const fd_q4_cache* c) {
+  return {reinterpret_cast<unsigned char*>(c->k_codes), reinterpret_cast<unsigned char*>(c->k_scales), reinterpret_cast<unsigned char*>(c->v_codes),
+          reinterpret_cast<fd::bf16_t*>(c->v_scales), (long long)c->stride_page, (long long)c->stride_head};
+}
+
+// What the attention and the commit over a cache in 4 bits ask of the scalar fields.
+static fd_status check_q4_args(const fd_attn_args* a) {
+  if (!a) return fail(FD_ERR_INVALID_ARG, "args is NULL");
+  if (a->batch < 0 || a->total_rows < 0 || a->max_kv_len < 0 || a->max_new_rows < 0 || a->num_pages < 0)
+    return fail(FD_ERR_INVALID_ARG, "negative size (batch %d, total_rows %d, max_kv_len %d, max_new_rows %d, num_pages %d)",
+                a->batch, a->total_rows, a->max_kv_len, a->max_new_rows, a->num_pages);
+  if (a->dtype == FD_F32) return fail(FD_ERR_UNSUPPORTED, "a cache in 4 bits goes with bf16 rows");
+  if (a->dtype != FD_BF16) return fail(FD_ERR_INVALID_ARG, "unknown dtype %d", a->dtype);
+  if (a->page_indices_len < 0) return fail(FD_ERR_INVALID_ARG, "page_indices_len %d is negative", a->page_indices_len);
+  if (a->batch > 65535) return fail(FD_ERR_UNSUPPORTED, "batch %d > 65535", a->batch);
+  if (a->max_kv_len > (1 << 30)) return fail(FD_ERR_UNSUPPORTED, "max_kv_len %d too large", a->max_kv_len);
+  return FD_OK;
+}
+
+static fd_status plan_attn_q4(const fd_attn_args* a, size_t* need) {
+  fd_status st = check_q4_args(a);
+  if (st != FD_OK) return st;
+  if (a->num_q_heads <= 0 || a->num_kv_heads <= 0 || a->num_q_heads % a->num_kv_heads)
+    return fail(FD_ERR_INVALID_ARG, "num_q_heads %d must be a positive multiple of num_kv_heads %d", a->num_q_heads, a->num_kv_heads);
+  if (a->head_dim != 128 && a->head_dim != 64) return fail(FD_ERR_UNSUPPORTED, "a cache in 4 bits has head_dim 128 or 64, not %d", a->head_dim);
+  if (a->flags & FD_ATTN_FORCE_GENERIC) return fail(FD_ERR_UNSUPPORTED, "there is no full-precision kernel over a cache in 4 bits");
+  if (!(a->sm_scale >= 0.f) || isinf(a->sm_scale)) return fail(FD_ERR_INVALID_ARG, "sm_scale must be finite and >= 0");
+  if (a->kv_chunk < 0 || a->kv_chunk % 64) return fail(FD_ERR_INVALID_ARG, "kv_chunk %d must be a non-negative multiple of 64", a->kv_chunk);
+  const int G = a->num_q_heads / a->num_kv_heads;
+  if ((long long)a->max_new_rows * G > (1 << 24)) return fail(FD_ERR_UNSUPPORTED, "max_new_rows x heads of a group above 2^24");
+  *need = fd::attn_q4_workspace(a->batch, a->num_kv_heads, G, a->total_rows, a->max_kv_len, a->max_new_rows, a->kv_chunk, a->head_dim);
+  if (*need == 0) return fail(FD_ERR_UNSUPPORTED, "batch x heads x rows x kv length too large for one launch");
+  return FD_OK;
+}
+
+size_t fd_verify_draft_attn_q4_workspace(const fd_attn_args* a) {
+  size_t need = 0;
+  return plan_attn_q4(a, &need) == FD_OK ? need : 0;
+}
+
+// The lengths, rows and page lists of a call, as the kernels take them.
+static fd::AttnParams q4_params(const fd_attn_args* a) {
+  fd::AttnParams p = {};
+  p.B = a->batch; p.Hq = a->num_q_heads; p.Hkv = a->num_kv_heads; p.D = a->head_dim;
+  p.G = a->num_q_heads > 0 ? a->num_q_heads / a->num_kv_heads : 1;
+  p.page_size = a->page_size;
+  p.total_rows = a->total_rows; p.max_kv_len = a->max_kv_len; p.max_new_rows = a->max_new_rows;
+  p.num_pages = a->num_pages; p.page_entries = a->page_indices_len;
+  p.sm_scale = a->sm_scale > 0.f ? a->sm_scale : 1.0f / sqrtf((float)a->head_dim);
+  p.page_indptr = a->page_indptr; p.page_indices = a->page_indices; p.kv_len = a->kv_len;
+  p.row_indptr = a->row_indptr; p.verify_len = a->verify_len; p.mask_vis = a->mask_vis; p.mask_blocks = a->mask_blocks;
+  p.q = a->q; p.k_new = a->k_new; p.v_new = a->v_new; p.out = a->out; p.lse = a->lse;
+  p.status = a->status;
+  return p;
+}
+
+fd_status fd_verify_draft_attn_q4(const fd_attn_args* a, const fd_q4_cache* cache, void* hip_stream) {
+  size_t need = 0;
+  fd_status st = plan_attn_q4(a, &need);
+  if (st != FD_OK) return st;
+  st = check_q4_cache(cache, a->head_dim, a->page_size, a->num_kv_heads);
+  if (st != FD_OK) return st;
+  g_err[0] = 0;
+  if (a->batch == 0 || a->total_rows == 0) return FD_OK;          // nothing to compute
+  if (!a->page_indptr || !a->kv_len || !a->row_indptr || !a->verify_len || !a->q || !a->k_new || !a->v_new || !a->out)
+    return fail(FD_ERR_INVALID_ARG, "a required device pointer is NULL");
+  if (a->max_kv_len > 0 && (!a->page_indices || a->num_pages == 0 || !q4_cache_complete(cache)))
+    return fail(FD_ERR_INVALID_ARG, "max_kv_len > 0 needs the cache's four arrays, page_indices and num_pages > 0");
+  if (a->max_new_rows == 0) return fail(FD_ERR_INVALID_ARG, "total_rows > 0 but max_new_rows == 0");
+  if (!a->workspace) return fail(FD_ERR_INVALID_ARG, "workspace is NULL");
+  if (a->workspace_bytes < need) return fail(FD_ERR_WORKSPACE_TOO_SMALL, "workspace %zu bytes, need %zu", a->workspace_bytes, need);
+  if (reinterpret_cast<uintptr_t>(a->workspace) & 255) return fail(FD_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+  if (!aligned16(a->q) || !aligned16(a->k_new) || !aligned16(a->v_new) || !aligned16(a->out))
+    return fail(FD_ERR_INVALID_ARG, "q, k_new, v_new and out must be 16-byte aligned");
+  hipError_t e = fd::run_attn_q4(q4_params(a), q4_cache(cache), a->workspace, a->kv_chunk, reinterpret_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return fail(FD_ERR_HIP, "attention kernel launch: %s", hipGetErrorString(e));
+  return FD_OK;
+}
+
+fd_status fd_append_kv_q4(const fd_attn_args* a, const fd_q4_cache* cache, const int32_t* accept_len, int32_t* kv_len_out, void* hip_stream) {
+  fd_status st = check_q4_args(a);
+  if (st != FD_OK) return st;
+  st = check_q4_cache(cache, a->head_dim, a->page_size, a->num_kv_heads);
+  if (st != FD_OK) return st;
+  if (a->max_new_rows > 65535) return fail(FD_ERR_UNSUPPORTED, "max_new_rows %d > 65535", a->max_new_rows);
+  g_err[0] = 0;
+  if (a->batch == 0) return FD_OK;
+  if (!accept_len || !kv_len_out || !a->kv_len || !a->row_indptr || !a->page_indptr || !a->verify_len)
+    return fail(FD_ERR_INVALID_ARG, "a required device pointer is NULL");
+  if (a->total_rows > 0 && a->max_new_rows > 0) {
+    if (!q4_cache_complete(cache) || !a->page_indices || !a->k_new || !a->v_new || a->num_pages == 0)
+      return fail(FD_ERR_INVALID_ARG, "the cache's four arrays, page_indices, k_new, v_new and num_pages > 0 are needed");
+    if (!aligned16(a->k_new) || !aligned16(a->v_new)) return fail(FD_ERR_INVALID_ARG, "k_new and v_new must be 16-byte aligned");
+  }
+  hipError_t e = fd::run_append_kv_q4(q4_params(a), q4_cache(cache), accept_len, kv_len_out, reinterpret_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return fail(FD_ERR_HIP, "append launch: %s", hipGetErrorString(e));
+  return FD_OK;
+}
+
+fd_status fd_read_kv_q4(const fd_q4_cache* cache, int32_t batch, int32_t num_kv_heads, int32_t head_dim, int32_t page_size,
+                        int32_t num_pages, const int32_t* page_indptr, const int32_t* page_indices, int32_t page_indices_len,
+                        const int32_t* start, const int32_t* out_indptr, int32_t total_rows, void* k_out, void* v_out,
+                        fd_dtype out_dtype, uint32_t* status, void* hip_stream) {
+  if (batch < 0 || num_pages < 0 || page_indices_len < 0 || total_rows < 0) return fail(FD_ERR_INVALID_ARG, "negative size");
+  if (batch > 65535) return fail(FD_ERR_UNSUPPORTED, "batch %d > 65535", batch);
+  if (out_dtype != FD_F32 && out_dtype != FD_BF16) return fail(FD_ERR_INVALID_ARG, "unknown dtype %d", (int)out_dtype);
+  fd_status st = check_q4_cache(cache, head_dim, page_size, num_kv_heads);
+  if (st != FD_OK) return st;
+  g_err[0] = 0;
+  if (batch == 0 || total_rows == 0) return FD_OK;
+  if (!q4_cache_complete(cache) || !page_indptr || !page_indices || !out_indptr || !k_out || !v_out || num_pages == 0)
+    return fail(FD_ERR_INVALID_ARG, "a required device pointer is NULL or num_pages is 0");
+  if (!aligned16(k_out) || !aligned16(v_out)) return fail(FD_ERR_INVALID_ARG, "k_out and v_out must be 16-byte aligned");
+  hipError_t e = fd::run_read_kv_q4(q4_cache(cache), batch, num_kv_heads, head_dim, page_size, num_pages, page_indptr, page_indices, page_indices_len,
+                                    start, out_indptr, total_rows, k_out, v_out, out_dtype, status, reinterpret_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return fail(FD_ERR_HIP, "read-back launch: %s", hipGetErrorString(e));
   return FD_OK;
 }
 

@@ -43,6 +43,37 @@ class fd_attn_args(C.Structure):
     ]
 
 
+class fd_table_args(C.Structure):
+    _fields_ = [
+        ("batch", C.c_int32), ("page_size", C.c_int32), ("table_stride", C.c_int32), ("total_rows", C.c_int32),
+        ("page_indices_len", C.c_int32), ("free_pages_len", C.c_int32),
+        ("kv_len", C.c_void_p), ("verify_len", C.c_void_p), ("mask_rows", C.c_void_p), ("mask_vis", C.c_void_p),
+        ("mask_blocks", C.c_void_p), ("block_table", C.c_void_p), ("table_len", C.c_void_p), ("table_len_out", C.c_void_p),
+        ("free_pages", C.c_void_p), ("free_count", C.c_void_p), ("free_count_out", C.c_void_p),
+        ("row_indptr", C.c_void_p), ("page_indptr", C.c_void_p), ("page_indices", C.c_void_p),
+        ("positions", C.c_void_p), ("slot_map", C.c_void_p), ("status", C.c_void_p),
+    ]
+
+
+class fd_rope_args(C.Structure):
+    _fields_ = [
+        ("total_rows", C.c_int32), ("num_q_heads", C.c_int32), ("num_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+        ("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("dtype", C.c_int32), ("eps", C.c_float),
+        ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
+        ("q_stride_row", C.c_int64), ("q_stride_head", C.c_int64), ("k_stride_row", C.c_int64), ("k_stride_head", C.c_int64),
+        ("v_stride_row", C.c_int64), ("v_stride_head", C.c_int64),
+        ("q_out", C.c_void_p), ("k_out", C.c_void_p), ("v_out", C.c_void_p),
+        ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("inv_freq", C.c_void_p), ("positions", C.c_void_p),
+    ]
+
+
+class fd_q4_cache(C.Structure):
+    _fields_ = [
+        ("k_codes", C.c_void_p), ("k_scales", C.c_void_p), ("v_codes", C.c_void_p), ("v_scales", C.c_void_p),
+        ("stride_page", C.c_int64), ("stride_head", C.c_int64),
+    ]
+
+
 class FlexDraftError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"{STATUS_NAMES.get(code, code)}: {msg}")
@@ -53,7 +84,8 @@ _lib = None
 
 EXPORTS = ["fd_verify_draft_attn_workspace", "fd_verify_draft_attn", "fd_accept_greedy", "fd_accept_sample",
            "fd_accept_workspace", "fd_draft_select", "fd_draft_select_workspace", "fd_append_kv", "fd_select_branch", "fd_last_error", "fd_version", "fd_verify_draft_attn_static",
-           "fd_verify_draft_plan"]
+           "fd_verify_draft_plan", "fd_step_tables", "fd_qk_norm_rope", "fd_verify_draft_attn_q4", "fd_verify_draft_attn_q4_workspace",
+           "fd_append_kv_q4", "fd_read_kv_q4"]
 
 
 def load() -> C.CDLL:
@@ -94,6 +126,19 @@ def load() -> C.CDLL:
     lib.fd_verify_draft_attn_static.argtypes = [C.POINTER(fd_attn_args), C.c_void_p]
     lib.fd_select_branch.restype = C.c_int
     lib.fd_select_branch.argtypes = [C.c_void_p] * 6 + [C.c_int32] * 3 + [C.c_void_p] * 3
+    lib.fd_step_tables.restype = C.c_int
+    lib.fd_step_tables.argtypes = [C.POINTER(fd_table_args), C.c_void_p]
+    lib.fd_qk_norm_rope.restype = C.c_int
+    lib.fd_qk_norm_rope.argtypes = [C.POINTER(fd_rope_args), C.c_void_p]
+    lib.fd_verify_draft_attn_q4_workspace.restype = C.c_size_t
+    lib.fd_verify_draft_attn_q4_workspace.argtypes = [C.POINTER(fd_attn_args)]
+    lib.fd_verify_draft_attn_q4.restype = C.c_int
+    lib.fd_verify_draft_attn_q4.argtypes = [C.POINTER(fd_attn_args), C.POINTER(fd_q4_cache), C.c_void_p]
+    lib.fd_append_kv_q4.restype = C.c_int
+    lib.fd_append_kv_q4.argtypes = [C.POINTER(fd_attn_args), C.POINTER(fd_q4_cache), C.c_void_p, C.c_void_p, C.c_void_p]
+    lib.fd_read_kv_q4.restype = C.c_int
+    lib.fd_read_kv_q4.argtypes = [C.POINTER(fd_q4_cache)] + [C.c_int32] * 5 + [C.c_void_p] * 2 + [C.c_int32] + [C.c_void_p] * 2 + \
+        [C.c_int32, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p]
     lib.fd_last_error.restype = C.c_char_p
     lib.fd_version.restype = C.c_char_p
     _lib = lib
@@ -266,6 +311,160 @@ def fd_select_branch(block_tokens, block_indptr, mask_blocks, accept_len, out_to
         None if verify_len is None else _ptr(_i32(verify_len, "verify_len")), B, block_tokens.numel(),
         out_tokens.shape[1], _ptr(_i32(out_tokens, "out_tokens")),
         None if out_block is None else _ptr(_i32(out_block, "out_block")), _stream(stream)))
+
+
+def _opt_i32(t: Optional[torch.Tensor], name: str):
+    return None if t is None else _i32(t, name).data_ptr()
+
+
+def make_table_args(kv_len, verify_len, block_table, table_len, free_pages, free_count, mask_rows=None, mask_vis=None, mask_blocks=None, *,
+                    page_size: int, row_indptr, page_indptr, page_indices, positions=None, slot_map=None, table_len_out=None,
+                    free_count_out=None, status=None):
+    """Fill an fd_table_args from tensors.  table_len_out / free_count_out default to table_len / free_count, updated in place."""
+    B = kv_len.shape[0]
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise TypeError("block_table must be [batch, entries]")
+    sizes = [("verify_len", verify_len, B), ("table_len", table_len, B), ("mask_rows", mask_rows, B), ("mask_vis", mask_vis, B),
+             ("mask_blocks", mask_blocks, B), ("table_len_out", table_len_out, B), ("row_indptr", row_indptr, B + 1), ("page_indptr", page_indptr, B + 1),
+             ("free_count", free_count, 1), ("free_count_out", free_count_out, 1)]
+    for name, t, n in sizes:
+        if t is not None and t.numel() != n:
+            raise TypeError(f"{name} must have {n} entries")
+    if slot_map is not None and (slot_map.dtype != torch.int64 or not slot_map.is_contiguous()):
+        raise TypeError("slot_map must be a contiguous int64 tensor")
+    rows = [t.numel() for t in (positions, slot_map) if t is not None]
+    a = fd_table_args()
+    a.batch = B; a.page_size = int(page_size); a.table_stride = block_table.shape[1]
+    # without positions and slots there is nothing to bound the rows by but the call's own limit
+    a.total_rows = min(rows) if rows else 1 << 20
+    a.page_indices_len = page_indices.numel(); a.free_pages_len = free_pages.numel()
+    a.kv_len = _i32(kv_len, "kv_len").data_ptr(); a.verify_len = _i32(verify_len, "verify_len").data_ptr()
+    a.mask_rows = _opt_i32(mask_rows, "mask_rows"); a.mask_vis = _opt_i32(mask_vis, "mask_vis")
+    a.mask_blocks = _opt_i32(mask_blocks, "mask_blocks")
+    a.block_table = _i32(block_table, "block_table").data_ptr()
+    a.table_len = _i32(table_len, "table_len").data_ptr()
+    a.table_len_out = _i32(table_len if table_len_out is None else table_len_out, "table_len_out").data_ptr()
+    a.free_pages = _i32(free_pages, "free_pages").data_ptr(); a.free_count = _i32(free_count, "free_count").data_ptr()
+    a.free_count_out = _i32(free_count if free_count_out is None else free_count_out, "free_count_out").data_ptr()
+    a.row_indptr = _i32(row_indptr, "row_indptr").data_ptr(); a.page_indptr = _i32(page_indptr, "page_indptr").data_ptr()
+    a.page_indices = _i32(page_indices, "page_indices").data_ptr()
+    a.positions = _opt_i32(positions, "positions"); a.slot_map = _ptr(slot_map)
+    a.status = None if status is None else status.data_ptr()
+    return a
+
+
+def fd_step_tables(args: fd_table_args, stream=None) -> None:
+    """Pages of a step change hands, then its row offsets, page lists, positions and slots are written."""
+    _check(load().fd_step_tables(C.byref(args), _stream(stream)))
+
+
+def fd_qk_norm_rope(q, k, q_out, k_out, positions, inv_freq, *, q_weight=None, k_weight=None, v=None, v_out=None, eps: float = 1e-6,
+                    interleaved: bool = False, stream=None) -> None:
+    """q [R, Hq, D], k (and v) [R, Hkv, D]: any strides between rows and heads; outputs dense.  rotary_dim is twice the number of
+    inv_freq's entries (None: no rotation)."""
+    R, Hq, D = q.shape
+    Hkv = k.shape[1]
+    for name, t, heads in (("q", q, Hq), ("k", k, Hkv), ("v", v, Hkv), ("q_out", q_out, Hq), ("k_out", k_out, Hkv), ("v_out", v_out, Hkv)):
+        if t is None:
+            continue
+        if tuple(t.shape) != (R, heads, D) or t.dtype != q.dtype or (t.numel() and t.stride(2) != 1):
+            raise TypeError(f"{name} must be [{R}, {heads}, {D}] of {q.dtype} with a contiguous last dimension")
+        if name.endswith("_out") and not t.is_contiguous():
+            raise TypeError(f"{name} must be contiguous")
+    for name, t in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if t is not None and (t.numel() != D or t.dtype != q.dtype or not t.is_contiguous()):
+            raise TypeError(f"{name} must be {D} contiguous elements of {q.dtype}")
+    if inv_freq is not None and (inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous()):
+        raise TypeError("inv_freq must be contiguous float32")
+    if inv_freq is not None and inv_freq.numel() and (positions is None or positions.numel() != R):
+        raise TypeError(f"positions must have {R} entries")
+    a = fd_rope_args()
+    a.total_rows = R; a.num_q_heads = Hq; a.num_kv_heads = Hkv; a.head_dim = D
+    a.rotary_dim = 0 if inv_freq is None else 2 * inv_freq.numel()
+    a.interleaved = 1 if interleaved else 0; a.dtype = _dtype_code(q); a.eps = float(eps)
+    a.q = q.data_ptr(); a.k = k.data_ptr(); a.v = _ptr(v)
+    a.q_stride_row, a.q_stride_head = q.stride(0), q.stride(1)
+    a.k_stride_row, a.k_stride_head = k.stride(0), k.stride(1)
+    if v is not None:
+        a.v_stride_row, a.v_stride_head = v.stride(0), v.stride(1)
+    a.q_out = q_out.data_ptr(); a.k_out = k_out.data_ptr(); a.v_out = _ptr(v_out)
+    a.q_weight = _ptr(q_weight); a.k_weight = _ptr(k_weight); a.inv_freq = _ptr(inv_freq)
+    a.positions = _opt_i32(positions, "positions")
+    _check(load().fd_qk_norm_rope(C.byref(a), _stream(stream)))
+
+
+class Q4Cache:
+    """The four tensors of a cache held in 4 bits (fd_q4_cache has the layout) and the struct over them."""
+
+    def __init__(self, k_codes, k_scales, v_codes, v_scales):
+        P, H, ps, half = k_codes.shape
+        D = 2 * half
+        want = (("k_codes", k_codes, (P, H, ps, D // 2), torch.uint8), ("k_scales", k_scales, (P, H, ps, D // 32), torch.uint8),
+                ("v_codes", v_codes, (P, H, ps // 16, 8 * D), torch.uint8), ("v_scales", v_scales, (P, H, ps), torch.bfloat16))
+        for name, t, shape, dtype in want:
+            if tuple(t.shape) != shape or t.dtype != dtype:
+                raise TypeError(f"{name} must be {dtype} of shape {shape}")
+            block = 1
+            for n, st in zip(reversed(shape[2:]), reversed(t.stride()[2:])):
+                if n > 1 and st != block:
+                    raise TypeError(f"{name}: the block of a page and head must be contiguous")
+                block *= n
+            if t.numel() and (t.stride(0) % block or t.stride(1) % block or (t.stride(0) // block, t.stride(1) // block) !=
+                              (k_codes.stride(0) // (ps * half), k_codes.stride(1) // (ps * half))):
+                raise TypeError(f"{name}: pages and heads must lie as those of k_codes do, in blocks")
+        self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
+        self.num_pages, self.num_kv_heads, self.page_size, self.head_dim = P, H, ps, D
+        self.c = fd_q4_cache(k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr(),
+                             k_codes.stride(0) // max(1, ps * half), k_codes.stride(1) // max(1, ps * half))
+
+
+def alloc_q4_cache(num_pages: int, num_kv_heads: int, page_size: int, head_dim: int, device="cuda") -> Q4Cache:
+    """A cache in 4 bits whose slots hold zeros."""
+    z = lambda *shape: torch.zeros(shape, dtype=torch.uint8, device=device)  # noqa: E731
+    return Q4Cache(z(num_pages, num_kv_heads, page_size, head_dim // 2), z(num_pages, num_kv_heads, page_size, head_dim // 32),
+                   z(num_pages, num_kv_heads, page_size // 16, 8 * head_dim),
+                   torch.zeros(num_pages, num_kv_heads, page_size, dtype=torch.bfloat16, device=device))
+
+
+def make_attn_args_q4(q, k_new, v_new, cache: Q4Cache, page_indptr, page_indices, kv_len, row_indptr, verify_len, mask_vis=None,
+                      mask_blocks=None, *, out, lse=None, max_kv_len: int, max_new_rows: int, sm_scale: float = 0.0, flags: int = 0,
+                      kv_chunk: int = 0, workspace=None, status=None):
+    """make_attn_args for a cache in 4 bits: fd_verify_draft_attn_q4 and fd_append_kv_q4 take the cache beside the struct."""
+    if cache.num_kv_heads != k_new.shape[1] or cache.head_dim != q.shape[2]:
+        raise TypeError("the cache's heads or head dim are not those of the rows")
+    a = make_attn_args(q, k_new, v_new, cache.k_codes, cache.k_codes, page_indptr, page_indices, kv_len, row_indptr, verify_len, mask_vis,
+                       mask_blocks, out=out, lse=lse, max_kv_len=max_kv_len, max_new_rows=max_new_rows, sm_scale=sm_scale, flags=flags,
+                       kv_chunk=kv_chunk, workspace=workspace, status=status)
+    a.k_cache = a.v_cache = None
+    a.cache_stride_page = a.cache_stride_head = a.cache_stride_token = 0
+    return a
+
+
+def fd_verify_draft_attn_q4_workspace(args: fd_attn_args) -> int:
+    return int(load().fd_verify_draft_attn_q4_workspace(C.byref(args)))
+
+
+def fd_verify_draft_attn_q4(args: fd_attn_args, cache: Q4Cache, stream=None) -> None:
+    """Enqueue the attention call described by `args` over the 4-bit `cache`."""
+    _check(load().fd_verify_draft_attn_q4(C.byref(args), C.byref(cache.c), _stream(stream)))
+
+
+def fd_append_kv_q4(args: fd_attn_args, cache: Q4Cache, accept_len, kv_len_out, stream=None) -> None:
+    """Round and commit new rows 0 .. accept_len[i] of the call described by `args` to the 4-bit `cache`."""
+    _check(load().fd_append_kv_q4(C.byref(args), C.byref(cache.c), _ptr(_i32(accept_len, "accept_len")),
+                                  _ptr(_i32(kv_len_out, "kv_len_out")), _stream(stream)))
+
+
+def fd_read_kv_q4(cache: Q4Cache, page_indptr, page_indices, start, out_indptr, k_out, v_out, *, status=None, stream=None) -> None:
+    """Tokens start[i] .. of every sequence as rows out_indptr[i] .. of k_out / v_out [R, Hkv, D], float32 or bfloat16."""
+    shape = (k_out.shape[0], cache.num_kv_heads, cache.head_dim)
+    for name, t in (("k_out", k_out), ("v_out", v_out)):
+        if tuple(t.shape) != shape or not t.is_contiguous() or t.dtype != k_out.dtype:
+            raise TypeError(f"{name} must be contiguous, of shape {shape}, both of one dtype")
+    _check(load().fd_read_kv_q4(
+        C.byref(cache.c), out_indptr.shape[0] - 1, cache.num_kv_heads, cache.head_dim, cache.page_size, cache.num_pages,
+        _ptr(_i32(page_indptr, "page_indptr")), _ptr(_i32(page_indices, "page_indices")), page_indices.numel(), _opt_i32(start, "start"),
+        _ptr(_i32(out_indptr, "out_indptr")), k_out.shape[0], _ptr(k_out), _ptr(v_out), _dtype_code(k_out), _ptr(status), _stream(stream)))
 
 
 def fd_version() -> str:
