@@ -159,6 +159,15 @@ fd_status plan_attn(const fd_attn_args* a, AttnPlan* plan, size_t have = SIZE_MA
   return FD_OK;
 }
 
+void set_page_magic(fd::AttnParams& p) {
+  // with 2^(s-1) < d <= 2^s the magic ceil(2^(31+s) / d) fits 32 bits; e = magic d - 2^(31+s) < d <= 2^s, hence
+  // n e < 2^(31+s) for every n < 2^31 and floor(n magic / 2^(31+s)) = n / d
+  const unsigned long long d = (unsigned)p.page_size;
+  int sh = 0;
+  while ((1ull << sh) < d) ++sh;
+  const unsigned long long magic = ((1ull << (31 + sh)) + d - 1) / d;
+  p.page_magic = (unsigned)magic; p.page_magic_shift = sh > 0 ? sh - 1 : 0;
+}
 
 // ---- static scratch of fd_verify_draft_attn_static ---------------------------------------------
 // The array lives in device memory of every GPU the library's code object is loaded on, from then
@@ -232,15 +241,7 @@ static fd_status attn_call(const fd_attn_args* a, void* workspace, size_t worksp
   p.G = p.Hq / p.Hkv; p.page_size = a->page_size;
   p.total_rows = a->total_rows; p.max_kv_len = a->max_kv_len; p.max_new_rows = a->max_new_rows;
   p.num_pages = a->num_pages; p.page_entries = a->page_indices_len; p.chunk = plan.chunk; p.max_chunks = plan.max_chunks; p.row_tiles = plan.row_tiles;
-  {
-    // with 2^(s-1) < d <= 2^s the magic ceil(2^(31+s) / d) fits 32 bits; e = magic d - 2^(31+s) < d <= 2^s, hence
-    // n e < 2^(31+s) for every n < 2^31 and floor(n magic / 2^(31+s)) = n / d
-    const unsigned long long d = (unsigned)a->page_size;
-    int sh = 0;
-    while ((1ull << sh) < d) ++sh;
-    const unsigned long long magic = ((1ull << (31 + sh)) + d - 1) / d;
-    p.page_magic = (unsigned)magic; p.page_magic_shift = sh > 0 ? sh - 1 : 0;
-  }
+  set_page_magic(p);
   // Full-precision kernel: with more than two chunks per compute unit, if all were as long as the longest may be, the device cuts equal pieces (even_pieces says
   // why from there on); not where 32 tile rows or fewer leave the products aside (4 of 512..2048 keys, 16 rows 24.0 us, in pieces 25.4).
   // The automatic cut aims at 1024 chunks, so that where an item has three or more there are at most 511 items and 1533 chunks; the limits on
@@ -581,6 +582,7 @@ static fd::AttnParams q4_params(const fd_attn_args* a) {
   p.B = a->batch; p.Hq = a->num_q_heads; p.Hkv = a->num_kv_heads; p.D = a->head_dim;
   p.G = a->num_q_heads > 0 ? a->num_q_heads / a->num_kv_heads : 1;
   p.page_size = a->page_size;
+  set_page_magic(p);
   p.total_rows = a->total_rows; p.max_kv_len = a->max_kv_len; p.max_new_rows = a->max_new_rows;
   p.num_pages = a->num_pages; p.page_entries = a->page_indices_len;
   p.sm_scale = a->sm_scale > 0.f ? a->sm_scale : 1.0f / sqrtf((float)a->head_dim);

@@ -14,6 +14,7 @@
 // Which key a row of S^T stands for is free: row i = (b4 b3 b2 b1 b0) is key (b4 b2 b3 b1 b0), so that the sixteen scores that a lane holds
 // are two runs of eight keys, as the second product wants them.
 #include "kv_q4.h"
+#include <type_traits>
 
 namespace fd {
 
@@ -30,7 +31,7 @@ struct Q4Sched {
   int max_partials;         // partial slots in the workspace
   float* part_acc;          // [max_partials][128][D] un-normalised O
   float* part_ml;           // [max_partials][128][2] maximum (base 2), sum
-  int4* entries;            // [B * Hkv * rt_max]: pieces, first partial slot, first packed row, new rows
+  int2* entries;            // [B * Hkv * rt_max]: pieces, first partial slot
 };
 
 // Row blocks that the waves of a work-group share out, for an item of so many tile rows.
@@ -66,20 +67,24 @@ __device__ __forceinline__ long long q4_block_sum(long long v, long long* sh) {
   return sh[0] + sh[1] + sh[2] + sh[3];
 }
 
-struct Q4Piece { int seq, head, rt, piece, pieces, slot; };
+struct Q4Piece { int head, rt, piece, pieces, slot, item; SeqInfo s; };
 
 // Which piece work-group w takes: pieces are numbered by (sequence, head, item, piece).  Every thread calls this; false: none.
+// A thread keeps what it read of its sequence, and the one whose sequence it is hands it over through LDS.
 __device__ __forceinline__ bool q4_find(const AttnParams& p, const Q4Sched& sc, int w, Q4Piece& out) {
   __shared__ long long sh_sum[4];
   __shared__ int sh_w[4][2];
-  __shared__ int sh_found[8];
+  __shared__ int sh_found[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int rounds = (p.B + Q4_BLOCK - 1) / Q4_BLOCK;
   Q4Cut cut = {};
+  SeqInfo mine = {};
+  uint32_t bad = 0;
   auto load = [&](int c) {
     cut = Q4Cut{};
+    bad = 0;
     const int i = c * Q4_BLOCK + tid;
-    if (i < p.B) cut = q4_cut(p, load_seq_t<false>(p, i));
+    if (i < p.B) { mine = load_seq_t<false>(p, i, &bad); cut = q4_cut(p, mine); }
   };
   long long units = 0;
   for (int c = 0; c < rounds; ++c) {
@@ -92,10 +97,11 @@ __device__ __forceinline__ bool q4_find(const AttnParams& p, const Q4Sched& sc, 
   if (tid == 0) sh_found[0] = -1;
   for (int c = 0; c < rounds; ++c) {
     if (rounds > 1) load(c);
+    if (w == 0 && bad) flag_status(p.status, bad);         // (work-group 0 comes by every sequence before it finds its piece ...
     const int pf = q4_pieces(sc, cut.blocks, cut.full ? Q4_ROWS : 0, target), pt = q4_pieces(sc, cut.blocks, cut.tail_rows, target);
-    const int mine = p.Hkv * (cut.full * pf + pt);
+    const int pieces = p.Hkv * (cut.full * pf + pt);
     const int split = p.Hkv * (cut.full * (pf > 1 ? pf : 0) + (pt > 1 ? pt : 0));
-    const int it = wave_incl_scan(mine), st = wave_incl_scan(split);
+    const int it = wave_incl_scan(pieces), st = wave_incl_scan(split);
     __syncthreads();
     if (lane == 63) { sh_w[wave][0] = it; sh_w[wave][1] = st; }
     __syncthreads();
@@ -104,27 +110,27 @@ __device__ __forceinline__ bool q4_find(const AttnParams& p, const Q4Sched& sc, 
       if (q < wave) { b0 += sh_w[q][0]; s0 += sh_w[q][1]; }
       base += sh_w[q][0]; sbase += sh_w[q][1];
     }
-    const int begin = b0 + it - mine;
-    if (w >= begin && w < begin + mine) {
+    const int begin = b0 + it - pieces;
+    if (w >= begin && w < begin + pieces) {
       int x = w - begin, sl = s0 + st - split;
       const int per_head = cut.full * pf + pt, split_head = cut.full * (pf > 1 ? pf : 0) + (pt > 1 ? pt : 0);
       const int head = x / per_head;
       x -= head * per_head; sl += head * split_head;
-      int rt, pieces;
-      if (x < cut.full * pf) { rt = x / pf; x -= rt * pf; pieces = pf; sl += pf > 1 ? rt * pf : 0; }
-      else { rt = cut.full; x -= cut.full * pf; pieces = pt; sl += pf > 1 ? cut.full * pf : 0; }
-      sh_found[0] = c * Q4_BLOCK + tid; sh_found[1] = head; sh_found[2] = rt; sh_found[3] = x; sh_found[4] = pieces; sh_found[5] = sl;
+      int rt, n;
+      if (x < cut.full * pf) { rt = x / pf; x -= rt * pf; n = pf; sl += pf > 1 ? rt * pf : 0; }
+      else { rt = cut.full; x -= cut.full * pf; n = pt; sl += pf > 1 ? cut.full * pf : 0; }
+      const int i = c * Q4_BLOCK + tid;
+      sh_found[0] = (i * p.Hkv + head) * sc.rt_max + rt; sh_found[1] = head; sh_found[2] = rt; sh_found[3] = x; sh_found[4] = n; sh_found[5] = sl;
+      sh_found[6] = mine.L; sh_found[7] = mine.row0; sh_found[8] = mine.n; sh_found[9] = mine.k; sh_found[10] = mine.v; sh_found[11] = mine.nb;
+      sh_found[12] = mine.page0; sh_found[13] = mine.npages;
     }
-    if (w < base) break;                                   // (uniform)
+    if (w < base && w > 0) break;                          // (uniform; ... and by those behind it)
   }
   __syncthreads();
-  out.seq = __builtin_amdgcn_readfirstlane(sh_found[0]);
-  out.head = __builtin_amdgcn_readfirstlane(sh_found[1]);
-  out.rt = __builtin_amdgcn_readfirstlane(sh_found[2]);
-  out.piece = __builtin_amdgcn_readfirstlane(sh_found[3]);
-  out.pieces = __builtin_amdgcn_readfirstlane(sh_found[4]);
-  out.slot = __builtin_amdgcn_readfirstlane(sh_found[5]);
-  return out.seq >= 0;
+  auto found = [&](int k) { return __builtin_amdgcn_readfirstlane(sh_found[k]); };
+  out.item = found(0); out.head = found(1); out.rt = found(2); out.piece = found(3); out.pieces = found(4); out.slot = found(5);
+  out.s = SeqInfo{found(6), found(7), found(8), found(9), found(10), found(11), found(12), found(13)};
+  return out.item >= 0;
 }
 
 __device__ __forceinline__ bf16x8 as_bf16x8(u32x4 x) { return __builtin_bit_cast(bf16x8, x); }
@@ -160,74 +166,38 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
   const int l31 = lane & 31, h = lane >> 5;
   Q4Piece pc;
   if (!q4_find(p, sc, blockIdx.x, pc)) return;
-  const SeqInfo s = load_seq(p, pc.seq);
+  const SeqInfo& s = pc.s;
   const int rows = min(Q4_ROWS, s.n * p.G - pc.rt * Q4_ROWS);
-  const int RB = q4_row_blocks(rows), KS = 4 / RB;
-  const int rb = wave & (RB - 1), slot = wave / RB;
+  const int RB = q4_row_blocks(rows), ks_shift = RB == 1 ? 2 : RB == 2 ? 1 : 0, KS = 1 << ks_shift;
+  const int rb = wave & (RB - 1), slot = wave >> (2 - ks_shift);
   const int cached = (s.L + Q4_TK - 1) / Q4_TK, blocks = cached + (s.n + Q4_TK - 1) / Q4_TK;
   const int first = (int)((long long)blocks * pc.piece / pc.pieces), last = (int)((long long)blocks * (pc.piece + 1) / pc.pieces);
 
-  // ---- this lane's row and its query, as the second operand of S^T = K Q^T ----
-  const int tr = rb * 32 + l31;
-  const bool row_on = tr < rows;
-  const int ti = pc.rt * Q4_ROWS + (row_on ? tr : 0);
-  const int nr = ti / p.G, g = ti - nr * p.G;            // new row, query head of the group
-  const bf16_t* qrow = reinterpret_cast<const bf16_t*>(p.q) + ((long long)(s.row0 + nr) * p.Hq + pc.head * p.G + g) * DH;
-  u32x4 qf[STEPS];
-#pragma unroll
-  for (int t = 0; t < STEPS; ++t) {
-    const u32x4 x = *reinterpret_cast<const u32x4*>(qrow + 64 * (t / 4) + 32 * h + 8 * (t % 4));
-    qf[t] = row_on ? x : u32x4{0, 0, 0, 0};
-  }
-  const float scale2 = p.sm_scale * 1.44269504088896340736f;
-
-  f32x16 o[NC];
-#pragma unroll
-  for (int cc = 0; cc < NC; ++cc)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) o[cc][e] = 0.f;
-  float m = -3e38f, l = 0.f;
-
-  // scores (scaled, base 2) -> probabilities; the running maximum and sum, and what O has to shrink by
-  auto softmax = [&](f32x16& x) {
-    float top = x[0];
-#pragma unroll
-    for (int e = 1; e < 16; ++e) top = fmaxf(top, x[e]);
-    top = max_halves(top);
-    if (__any(top > m + Q4_LAZY)) {
-      const float mn = fmaxf(m, top), f = __builtin_amdgcn_exp2f(m - mn);
-      m = mn;
-      l *= f;
-#pragma unroll
-      for (int cc = 0; cc < NC; ++cc)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[cc][e] *= f;
-    }
-#pragma unroll
-    for (int e = 0; e < 16; ++e) { x[e] = __builtin_amdgcn_exp2f(x[e] - m); l += x[e]; }
-  };
-
-  // ---- cached keys ----
+  // ---- cached keys: which blocks, where they lie ----
   const int lo = first + slot, hi = min(last, cached);
-  // where sixteen keys lie: lane t knows it for the sixteens of this wave's blocks lo + KS (t / 2), t % 2
-  long long where = 0;
-  auto find_pages = [&](int b0) {
-    const int pos = 32 * (b0 + KS * (lane >> 1)) + 16 * (lane & 1);
-    where = 0;
-    if (pos < s.L) {
-      const int lp = pos / p.page_size;
-      int page = p.page_indices[s.page0 + lp];
-      if (page < 0 || page >= p.num_pages) { flag_status(p.status, FD_DEV_PAGE_RANGE); page = 0; }
-      where = q4_token(c, page, pc.head, p.page_size, pos - lp * p.page_size);
+  const int count = lo < hi ? (hi - lo + KS - 1) >> ks_shift : 0;        // blocks of this wave: lo, lo + KS, ...
+  // the pages of the wave's block t, sixteen keys each; past the last block, and for sixteen keys past the prefix, those of keys that are there
+  struct Pages { int page[2], slot[2]; };
+  auto find_pages = [&](int t) {
+    Pages r;
+    const int pos = 32 * (lo + (min(t, count - 1) << ks_shift));
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int x = q && pos + 16 < s.L ? pos + 16 : pos;
+      const int lp = (int)(__umulhi((unsigned)x, p.page_magic) >> p.page_magic_shift);
+      r.slot[q] = x - lp * p.page_size;
+      r.page[q] = sload(p.page_indices, s.page0 + lp);
     }
+    return r;
   };
-  auto lane_where = [&](int t) -> long long {
-    const unsigned a = __builtin_amdgcn_readlane((unsigned)where, t), b = __builtin_amdgcn_readlane((unsigned)((unsigned long long)where >> 32), t);
-    return (long long)(((unsigned long long)b << 32) | a);
+  auto token_of = [&](const Pages& r, int q) -> long long {
+    int page = r.page[q];
+    if (page < 0 || page >= p.num_pages) { if (lane == 0) flag_status(p.status, FD_DEV_PAGE_RANGE); page = 0; }
+    return q4_token(c, page, pc.head, p.page_size, r.slot[q]);
   };
   const int key_of_row = (l31 & 16) | ((l31 & 4) << 1) | ((l31 & 8) >> 1) | (l31 & 3);
-  auto request = [&](Q4Regs<DH>& r, int t) {             // t: which of the wave's blocks since find_pages
-    const long long w0 = lane_where(2 * t), w1 = lane_where(2 * t + 1);
+  auto request = [&](Q4Regs<DH>& r, const Pages& at) {
+    const long long w0 = token_of(at, 0), w1 = token_of(at, 1);
     const long long mine = (key_of_row & 16 ? w1 : w0) + (key_of_row & 15);
     const u32x4* k = reinterpret_cast<const u32x4*>(c.k_codes + mine * (DH / 2)) + h;
 #pragma unroll
@@ -249,7 +219,60 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
       r.vs[q] = *reinterpret_cast<const u32x4*>(c.v_scales + w + 8 * h);
     }
   };
-  auto multiply = [&](const Q4Regs<DH>& r, int b) {
+  Q4Regs<DH> ra, rb_;
+  Pages pa = {}, pb = {};
+  if (count > 0) { pa = find_pages(0); pb = find_pages(1); }
+
+  // ---- this lane's row and its query, as the second operand of S^T = K Q^T ----
+  const int tr = rb * 32 + l31;
+  const bool row_on = tr < rows;
+  const int ti = pc.rt * Q4_ROWS + (row_on ? tr : 0);
+  const int nr = ti / p.G, g = ti - nr * p.G;            // new row, query head of the group
+  const bf16_t* qrow = reinterpret_cast<const bf16_t*>(p.q) + ((long long)(s.row0 + nr) * p.Hq + pc.head * p.G + g) * DH;
+  u32x4 qf[STEPS];
+#pragma unroll
+  for (int t = 0; t < STEPS; ++t) qf[t] = *reinterpret_cast<const u32x4*>(qrow + 64 * (t / 4) + 32 * h + 8 * (t % 4));
+  if (count > 0) {
+    request(ra, pa);
+    if (count > 1) request(rb_, pb);
+    pa = find_pages(2); pb = find_pages(3);
+  }
+#pragma unroll
+  for (int t = 0; t < STEPS; ++t)
+    if (!row_on) qf[t] = u32x4{0, 0, 0, 0};
+  const float scale2 = p.sm_scale * 1.44269504088896340736f;
+
+  f32x16 o[NC];
+#pragma unroll
+  for (int cc = 0; cc < NC; ++cc)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[cc][e] = 0.f;
+  float m = -3e38f, l = 0.f;                             // running maximum (scaled, base 2) and sum
+
+  // scores -> probabilities; the running maximum and sum, and what O has to shrink by
+  auto softmax = [&](f32x16& x) {
+    float t[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) t[e] = fmaxf(fmaxf(x[4 * e], x[4 * e + 1]), fmaxf(x[4 * e + 2], x[4 * e + 3]));
+    const float top = max_halves(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]))) * scale2;
+    if (__any(top > m + Q4_LAZY)) {
+      const float mn = fmaxf(m, top), f = __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= f;
+#pragma unroll
+      for (int cc = 0; cc < NC; ++cc)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[cc][e] *= f;
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], scale2, -m));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) t[e] = (x[4 * e] + x[4 * e + 1]) + (x[4 * e + 2] + x[4 * e + 3]);
+    l += (t[0] + t[1]) + (t[2] + t[3]);
+  };
+  // left: keys of the block, at least 32 unless MASKED
+  auto multiply = [&](const Q4Regs<DH>& r, int left, auto masked) {
+    constexpr bool MASKED = decltype(masked)::value;
     f32x16 x;
 #pragma unroll
     for (int e = 0; e < 16; ++e) x[e] = 0.f;
@@ -258,10 +281,7 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
       const float ks = q4_key_scale((r.ks >> (8 * (2 * (t / 4) + h))) & 255u);
       x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(q4_to_bf16(r.k[t / 4][t % 4], ks)), as_bf16x8(qf[t]), x, 0, 0, 0);
     }
-    const int left = s.L - 32 * b;                       // keys of this block, if below 32
-#pragma unroll
-    for (int e = 0; e < 16; ++e) x[e] *= scale2;
-    if (left < 32) {
+    if (MASKED) {
 #pragma unroll
       for (int e = 0; e < 16; ++e)
         if (16 * (e / 8) + 8 * h + e % 8 >= left) x[e] = -INFINITY;
@@ -274,7 +294,7 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         float p0 = x[8 * q + 2 * e] * __uint_as_float(r.vs[q][e] << 16), p1 = x[8 * q + 2 * e + 1] * __uint_as_float(r.vs[q][e] & 0xffff0000u);
-        if (left < 32) {
+        if (MASKED) {
           if (16 * q + 8 * h + 2 * e >= left) p0 = 0.f;
           if (16 * q + 8 * h + 2 * e + 1 >= left) p1 = 0.f;
         }
@@ -285,84 +305,94 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
         o[cc] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(q4_to_bf16(r.v[q][cc], 1.f)), as_bf16x8(pf), o[cc], 0, 0, 0);
     }
   };
-  if (lo < hi) {
-    const int count = (hi - lo + KS - 1) / KS;           // blocks of this wave
-    for (int c0 = 0; c0 < count; c0 += 32) {
-      find_pages(lo + KS * c0);
-      const int n = min(32, count - c0);
-      Q4Regs<DH> now, next;
-      request(now, 0);
-      for (int t = 0; t < n; ++t) {
-        if (t + 1 < n) request(next, t + 1);
-        multiply(now, lo + KS * (c0 + t));
-        now = next;
-      }
+  // Two blocks are held, a third and a fourth are looked up.  Only the last block can be ragged, so the loop, which leaves one to three, masks nothing.
+  if (count > 0) {
+    constexpr std::false_type whole; constexpr std::true_type ragged;
+    auto left = [&](int t) { return s.L - 32 * (lo + (t << ks_shift)); };
+    int t = 0;
+    for (; t + 3 < count; t += 2) {
+      multiply(ra, 32, whole);
+      request(ra, pa);
+      pa = find_pages(t + 4);
+      multiply(rb_, 32, whole);
+      request(rb_, pb);
+      pb = find_pages(t + 5);
     }
+    multiply(ra, left(t), ragged);
+    if (t + 2 < count) request(ra, pa);
+    if (t + 1 < count) multiply(rb_, left(t + 1), ragged);
+    if (t + 2 < count) multiply(ra, left(t + 2), ragged);
   }
 
   // ---- the sequence's own rows, in bf16 ----
   {
     int b = first > cached ? first : cached;             // the wave's first block at or behind `cached`
-    b += ((slot - (b - first)) % KS + KS) % KS;
+    b += (slot - (b - first)) & (KS - 1);
     const RowWindow win = row_window(nr, s);
+    const long long stride = (long long)p.Hkv * DH;
+    const bf16_t* k0 = reinterpret_cast<const bf16_t*>(p.k_new) + s.row0 * stride + (long long)pc.head * DH;
+    const bf16_t* v0 = reinterpret_cast<const bf16_t*>(p.v_new) + s.row0 * stride + (long long)pc.head * DH;
     for (; b < last; b += KS) {
       const int t0 = 32 * (b - cached);
-      const int key = t0 + key_of_row;
-      const long long stride = (long long)p.Hkv * DH;
-      const bf16_t* krow = reinterpret_cast<const bf16_t*>(p.k_new) + (s.row0 + (key < s.n ? key : 0)) * stride + (long long)pc.head * DH;
+      const bf16_t* krow = k0 + min(t0 + key_of_row, s.n - 1) * stride;         // (behind the last row: that row, which the mask below leaves out)
       f32x16 x;
 #pragma unroll
       for (int e = 0; e < 16; ++e) x[e] = 0.f;
 #pragma unroll
       for (int t = 0; t < STEPS; ++t) {
-        u32x4 kf = *reinterpret_cast<const u32x4*>(krow + 64 * (t / 4) + 32 * h + 8 * (t % 4));
-        if (key >= s.n) kf = u32x4{0, 0, 0, 0};
+        const u32x4 kf = *reinterpret_cast<const u32x4*>(krow + 64 * (t / 4) + 32 * h + 8 * (t % 4));
         x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kf), as_bf16x8(qf[t]), x, 0, 0, 0);
       }
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const int t = t0 + 16 * (e / 8) + 8 * h + e % 8;
-        x[e] = t < s.n && new_key_visible(win, t) ? x[e] * scale2 : -INFINITY;
+        x[e] = ((t < s.n) & new_key_visible(win, t)) ? x[e] : -INFINITY;
       }
       softmax(x);
-      const bf16_t* v0 = reinterpret_cast<const bf16_t*>(p.v_new) + s.row0 * stride + (long long)pc.head * DH;
+      // A value that is no number must not reach a row that does not see it, and zero times it is NaN: it enters the product as zero.
+      bool odd = false;
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
         u32x4 pf;
 #pragma unroll
         for (int e = 0; e < 4; ++e) pf[e] = pack_bf16x2(x[8 * q + 2 * e], x[8 * q + 2 * e + 1]);
-        bool odd = false;                                // a value that is no number: it must not reach a row that does not see it
+        const bf16_t* vt[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) vt[e] = v0 + min(t0 + 16 * q + 8 * h + e, s.n - 1) * stride + l31;
 #pragma unroll
         for (int cc = 0; cc < NC; ++cc) {
-          u32x4 vf;
+          unsigned v[8];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int ta = t0 + 16 * q + 8 * h + 2 * e;
-            unsigned va = ta < s.n ? v0[ta * stride + 32 * cc + l31] : 0u, vb = ta + 1 < s.n ? v0[(ta + 1) * stride + 32 * cc + l31] : 0u;
-            if ((va & 0x7f80u) == 0x7f80u) { odd = true; va = 0; }
-            if ((vb & 0x7f80u) == 0x7f80u) { odd = true; vb = 0; }
-            vf[e] = va | (vb << 16);
+          for (int e = 0; e < 8; ++e) {
+            v[e] = vt[e][32 * cc];
+            const bool bad = (v[e] & 0x7f80u) == 0x7f80u;
+            odd |= bad;
+            v[e] = bad ? 0u : v[e];
           }
+          const u32x4 vf = {v[0] | (v[1] << 16), v[2] | (v[3] << 16), v[4] | (v[5] << 16), v[6] | (v[7] << 16)};
           o[cc] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vf), as_bf16x8(pf), o[cc], 0, 0, 0);
         }
-        if (__any(odd)) {                                // rare: infinities and NaN are added one by one where they are seen
+      }
+      if (__any(odd)) {                                  // rare: infinities and NaN are added one by one where they are seen
+        float* mine = &lds_o[wave][l31][0];              // (this wave's part of LDS, free until the end; a row's 32 probabilities)
 #pragma unroll
-          for (int w = 0; w < 4; ++w)                    // a word of P: two keys of either half
-            for (int u = 0; u < 4; ++u) {
-              const int t = t0 + 16 * q + 8 * (u >> 1) + 2 * w + (u & 1);
-              if (t >= s.n) continue;
-              const unsigned pw = __shfl((int)pf[w], (u >> 1) * 32 + l31);
-              const float pr = __uint_as_float(u & 1 ? pw & 0xffff0000u : pw << 16);
-              if (!new_key_visible(win, t)) continue;
+        for (int e = 0; e < 16; ++e) mine[16 * (e / 8) + 8 * h + e % 8] = x[e];
+        __builtin_amdgcn_wave_barrier();
+        const int n = min(32, s.n - t0);
+#pragma unroll 1
+        for (int t = 0; t < n; ++t) {
+          if (!new_key_visible(win, t0 + t)) continue;
+          const float pr = mine[t];
+          const bf16_t* vrow = v0 + (t0 + t) * stride + 4 * h;
 #pragma unroll
-              for (int cc = 0; cc < NC; ++cc)
+          for (int cc = 0; cc < NC; ++cc)
 #pragma unroll
-                for (int a = 0; a < 16; ++a) {
-                  const float v = bf16_to_f32(v0[t * stride + 32 * cc + 8 * (a / 4) + 4 * h + a % 4]);
-                  if (!(fabsf(v) < INFINITY)) o[cc][a] += pr * v;
-                }
+            for (int a = 0; a < 16; ++a) {
+              const float v = bf16_to_f32(vrow[32 * cc + 8 * (a / 4) + a % 4]);
+              if (!(fabsf(v) < INFINITY)) o[cc][a] += pr * v;
             }
         }
+        __builtin_amdgcn_wave_barrier();
       }
     }
   }
@@ -378,8 +408,7 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
       *reinterpret_cast<f32x4*>(&lds_o[wave][l31][32 * cc + 8 * q + 4 * h]) = x;
     }
   __syncthreads();
-  const int item = (pc.seq * p.Hkv + pc.head) * sc.rt_max + pc.rt;
-  if (threadIdx.x == 0 && pc.piece == 0) sc.entries[item] = make_int4(pc.pieces, pc.slot, s.row0, s.n);
+  if (threadIdx.x == 0 && pc.piece == 0) sc.entries[pc.item] = make_int2(pc.pieces, pc.slot);
   constexpr int TPR = 8, CPT = DH / TPR;                 // threads of a row, channels of a thread
   const int part = threadIdx.x % TPR;
   for (int r = threadIdx.x / TPR; r < rows; r += Q4_BLOCK / TPR) {
@@ -401,51 +430,79 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
       }
     }
     if (pc.pieces > 1) {
-      if (pc.slot + pc.piece >= sc.max_partials) continue;           // (cannot be: the workspace holds every split piece)
+      if (pc.slot + pc.piece >= sc.max_partials) continue;           // (only where the device's rows contradict the host's bounds)
       const long long at = (long long)(pc.slot + pc.piece) * Q4_ROWS + r;
       float* dst = sc.part_acc + at * DH + part * CPT;
 #pragma unroll
       for (int e = 0; e < CPT; e += 4) *reinterpret_cast<f32x4*>(dst + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
-      if (part == 0) { sc.part_ml[at * 2] = M; sc.part_ml[at * 2 + 1] = sum; }
+      if (part == 0) *reinterpret_cast<float2*>(sc.part_ml + at * 2) = make_float2(M, sum);
     } else {
       const int t = pc.rt * Q4_ROWS + r, n = t / p.G;
       const long long orow = (long long)(s.row0 + n) * p.Hq + pc.head * p.G + (t - n * p.G);
       const float inv = 1.f / sum;
-      unsigned* dst = reinterpret_cast<unsigned*>(reinterpret_cast<bf16_t*>(p.out) + orow * DH + part * CPT);
+      u32x4* dst = reinterpret_cast<u32x4*>(reinterpret_cast<bf16_t*>(p.out) + orow * DH + part * CPT);
 #pragma unroll
-      for (int e = 0; e < CPT; e += 2) dst[e / 2] = pack_bf16x2(acc[e] * inv, acc[e + 1] * inv);
+      for (int e = 0; e < CPT; e += 8)
+        dst[e / 8] = u32x4{pack_bf16x2(acc[e] * inv, acc[e + 1] * inv), pack_bf16x2(acc[e + 2] * inv, acc[e + 3] * inv),
+                           pack_bf16x2(acc[e + 4] * inv, acc[e + 5] * inv), pack_bf16x2(acc[e + 6] * inv, acc[e + 7] * inv)};
       if (part == 0 && p.lse) p.lse[orow] = (M + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
     }
   }
 }
 
-// Merge of the partials of split items, by rows: a row is taken by DH / 8 lanes.
+// Merge of the partials of split items, by rows: a row is taken by TPR = DH / 8 lanes, eight channels each.  TPR pieces at a time: lane j
+// reads the maximum and sum of piece j, so that they are one latency, and the rows' values are requested four pieces at once.
 template <int DH>
 __global__ __launch_bounds__(256) void attn_q4_combine_kernel(AttnParams p, Q4Sched sc) {
-  constexpr int TPR = DH / 8, RPB = 256 / TPR;
+  constexpr int TPR = DH / 8, RPB = 256 / TPR, AT_ONCE = 4;
   const int item = blockIdx.x, rt = item % sc.rt_max, head = item / sc.rt_max % p.Hkv, seq = item / sc.rt_max / p.Hkv;
-  // (a sequence without new rows, or with fewer, has no such item and no entry)
-  const SeqInfo s = load_seq(p, seq);
-  const int rows = min(Q4_ROWS, s.n * p.G - rt * Q4_ROWS);
+  const int2 e = sc.entries[item];
+  // (a sequence without new rows, or with fewer, has no such item: what stands in its entry is old)
+  const int r0 = sload(p.row_indptr, seq), r1 = sload(p.row_indptr, seq + 1);
+  const int row0 = clampi(r0, 0, p.total_rows), new_rows = min(clampi(r1 - r0, 0, p.max_new_rows), p.total_rows - row0);
+  const int rows = min(Q4_ROWS, new_rows * p.G - rt * Q4_ROWS);
+  const int pieces = __builtin_amdgcn_readfirstlane(e.x), slot = __builtin_amdgcn_readfirstlane(e.y);
   const int r = blockIdx.y * RPB + threadIdx.x / TPR, part = threadIdx.x % TPR;
-  if (rows <= 0 || blockIdx.y * RPB >= rows) return;
-  const int4 e = sc.entries[item];
-  const int pieces = e.x, slot = e.y;
-  if (pieces <= 1 || r >= rows || slot < 0 || (long long)slot + pieces > sc.max_partials) return;
-  float M = -3e38f;
-  for (int q = 0; q < pieces; ++q) M = fmaxf(M, sc.part_ml[((long long)(slot + q) * Q4_ROWS + r) * 2]);
-  float acc[8] = {}, sum = 0.f;
-  for (int q = 0; q < pieces; ++q) {
-    const long long at = (long long)(slot + q) * Q4_ROWS + r;
-    const float f = __builtin_amdgcn_exp2f(sc.part_ml[at * 2] - M);
-    sum += f * sc.part_ml[at * 2 + 1];
-    const f32x4* src = reinterpret_cast<const f32x4*>(sc.part_acc + at * DH + part * 8);
-    const f32x4 x = src[0], y = src[1];
+  if ((int)blockIdx.y * RPB >= rows || pieces <= 1 || slot < 0 || (long long)slot + pieces > sc.max_partials) return;
+  const int rr = r < rows ? r : 0;                       // (every lane takes part in the exchanges)
+  float M = -3e38f, sum = 0.f, acc[8] = {};
+  for (int q0 = 0; q0 < pieces; q0 += TPR) {
+    const int n = min(TPR, pieces - q0);
+    const long long at = (long long)(slot + q0) * Q4_ROWS + rr;
+    float2 ml = make_float2(-3e38f, 0.f);
+    if (part < n) ml = *reinterpret_cast<const float2*>(sc.part_ml + (at + (long long)part * Q4_ROWS) * 2);
+    float top = ml.x;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) { acc[u] += f * x[u]; acc[4 + u] += f * y[u]; }
+    for (int d = 1; d < TPR; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+    const float mn = fmaxf(M, top), shrink = __builtin_amdgcn_exp2f(M - mn);
+    const float f = __builtin_amdgcn_exp2f(ml.x - mn);   // this lane's piece
+    float add = f * ml.y;
+#pragma unroll
+    for (int d = 1; d < TPR; d <<= 1) add += __shfl_xor(add, d);
+    M = mn;
+    sum = sum * shrink + add;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) acc[u] *= shrink;
+    const float* src = sc.part_acc + at * DH + part * 8;
+    for (int q = 0; q < n; q += AT_ONCE) {
+      f32x4 x[AT_ONCE][2];
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) {
+        const f32x4* y = reinterpret_cast<const f32x4*>(src + (long long)min(q + u, n - 1) * Q4_ROWS * DH);
+        x[u][0] = y[0]; x[u][1] = y[1];
+      }
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) {
+        if (q + u >= n) break;                           // (uniform; no zero times an infinity)
+        const float w = __shfl(f, (int)(threadIdx.x & 63) / TPR * TPR + q + u);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) { acc[v] += w * x[u][0][v]; acc[4 + v] += w * x[u][1][v]; }
+      }
+    }
   }
+  if (r >= rows) return;
   const int t = rt * Q4_ROWS + r, n = t / p.G;
-  const long long orow = (long long)(s.row0 + n) * p.Hq + head * p.G + (t - n * p.G);
+  const long long orow = (long long)(row0 + n) * p.Hq + head * p.G + (t - n * p.G);
   const float inv = 1.f / sum;
   u32x4 w;
 #pragma unroll
@@ -479,7 +536,7 @@ static Q4Shape q4_shape(int batch, int num_kv_heads, int group, int total_rows, 
   auto round = [](size_t x) { return (x + 255) / 256 * 256; };
   z.off_ml = round((size_t)z.partials * Q4_ROWS * head_dim * sizeof(float));
   z.off_entries = z.off_ml + round((size_t)z.partials * Q4_ROWS * 2 * sizeof(float));
-  z.total = z.off_entries + round((size_t)(batch > 0 ? batch : 1) * num_kv_heads * z.rt_max * sizeof(int4));
+  z.total = z.off_entries + round((size_t)(batch > 0 ? batch : 1) * num_kv_heads * z.rt_max * sizeof(int2));
   return z;
 }
 
@@ -493,7 +550,7 @@ size_t attn_q4_workspace(int batch, int num_kv_heads, int group, int total_rows,
 hipError_t run_attn_q4(const AttnParams& p, const Q4Cache& c, void* workspace, int kv_chunk, hipStream_t st) {
   const Q4Shape z = q4_shape(p.B, p.Hkv, p.G, p.total_rows, p.max_kv_len, p.max_new_rows, kv_chunk, p.D);
   char* ws = reinterpret_cast<char*>(workspace);
-  const Q4Sched sc = {z.fixed, z.rt_max, (int)z.partials, reinterpret_cast<float*>(ws), reinterpret_cast<float*>(ws + z.off_ml), reinterpret_cast<int4*>(ws + z.off_entries)};
+  const Q4Sched sc = {z.fixed, z.rt_max, (int)z.partials, reinterpret_cast<float*>(ws), reinterpret_cast<float*>(ws + z.off_ml), reinterpret_cast<int2*>(ws + z.off_entries)};
   if (z.wgs == 0) return hipSuccess;
   const int per_row = p.D / 8, most_rows = (int)((long long)p.max_new_rows * p.G < Q4_ROWS ? p.max_new_rows * p.G : Q4_ROWS);
   const dim3 grid((unsigned)((long long)p.B * p.Hkv * z.rt_max), (most_rows * per_row + 255) / 256);
