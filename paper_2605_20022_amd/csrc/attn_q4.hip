@@ -21,12 +21,13 @@ namespace fd {
 constexpr int Q4_BLOCK = 256;
 constexpr int Q4_TK = 32;                 // keys of a block
 constexpr int Q4_ROWS = 128;              // tile rows of an item
-constexpr float Q4_LAZY = 6.f;            // the softmax reference follows the row maximum in steps of at least 2^6
+constexpr float Q4_LAZY = 256.f;          // sum of a row's sixteen probabilities from which on the softmax reference follows the row maximum
 constexpr int Q4_PIECES = 1024;           // pieces aimed at
 constexpr int Q4_MIN_PIECE = 8;           // blocks of a piece, at least (but for the last of a short item)
 
 struct Q4Sched {
   int fixed;                // > 0: blocks of a piece, asked for by the caller
+  int unit_shift;           // work is counted in 2^unit_shift units
   int rt_max;               // items of a (sequence, head), at most
   int max_partials;         // partial slots in the workspace
   float* part_acc;          // [max_partials][128][D] un-normalised O
@@ -49,88 +50,64 @@ __device__ __forceinline__ Q4Cut q4_cut(const AttnParams& p, const SeqInfo& s) {
   return c;
 }
 // Pieces of an item of so many rows.  target: units of weight x blocks a piece should have.
-__device__ __forceinline__ int q4_pieces(const Q4Sched& sc, int blocks, int rows, long long target) {
+__device__ __forceinline__ int q4_pieces(const Q4Sched& sc, int blocks, int rows, int target) {
   if (blocks <= 0 || rows <= 0) return 0;
-  long long per = sc.fixed > 0 ? sc.fixed : (target + q4_weight(rows) - 1) / q4_weight(rows);
+  const unsigned w = q4_weight(rows);
+  unsigned per = sc.fixed > 0 ? (unsigned)sc.fixed : ((unsigned)target + w - 1) / w;
   if (sc.fixed <= 0 && per < Q4_MIN_PIECE) per = Q4_MIN_PIECE;
-  return (int)((blocks + per - 1) / per);
-}
-
-// One value summed over the work-group (all threads), exact for integers.
-__device__ __forceinline__ long long q4_block_sum(long long v, long long* sh) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
-  __syncthreads();
-  if (lane == 0) sh[wave] = v;
-  __syncthreads();
-  return sh[0] + sh[1] + sh[2] + sh[3];
+  return (int)(((unsigned)blocks + per - 1) / per);
 }
 
 struct Q4Piece { int head, rt, piece, pieces, slot, item; SeqInfo s; };
 
-// Which piece work-group w takes: pieces are numbered by (sequence, head, item, piece).  Every thread calls this; false: none.
-// A thread keeps what it read of its sequence, and the one whose sequence it is hands it over through LDS.
+// Which piece work-group w takes: pieces are numbered by (sequence, head, item, piece).  Every wave finds it by itself, a sequence a lane, 64 at a
+// time: the lengths are one latency of memory, the rest lane shifts, and no wave waits for another.  false: none.
 __device__ __forceinline__ bool q4_find(const AttnParams& p, const Q4Sched& sc, int w, Q4Piece& out) {
-  __shared__ long long sh_sum[4];
-  __shared__ int sh_w[4][2];
-  __shared__ int sh_found[16];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int rounds = (p.B + Q4_BLOCK - 1) / Q4_BLOCK;
+  const int lane = threadIdx.x & 63;
+  const int rounds = (p.B + 63) / 64;
   Q4Cut cut = {};
   SeqInfo mine = {};
-  uint32_t bad = 0;
   auto load = [&](int c) {
     cut = Q4Cut{};
-    bad = 0;
-    const int i = c * Q4_BLOCK + tid;
+    uint32_t bad = 0;
+    const int i = c * 64 + lane;
     if (i < p.B) { mine = load_seq_t<false>(p, i, &bad); cut = q4_cut(p, mine); }
+    if (bad && w == 0 && threadIdx.x < 64) flag_status(p.status, bad);        // (work-group 0 comes by every sequence)
   };
-  long long units = 0;
+  int total = 0;                                         // units of weight x blocks of one head, in 2^unit_shift (the host's bounds say that they fit)
   for (int c = 0; c < rounds; ++c) {
     load(c);
-    units += (long long)cut.blocks * p.Hkv * (cut.full * q4_weight(Q4_ROWS) + (cut.tail_rows ? q4_weight(cut.tail_rows) : 0));
+    const long long units = (long long)cut.blocks * (cut.full * q4_weight(Q4_ROWS) + (cut.tail_rows ? q4_weight(cut.tail_rows) : 0));
+    total += wave_total((int)((units + (1ll << sc.unit_shift) - 1) >> sc.unit_shift));      // (up, so that there are never more pieces than the host counts on)
   }
-  const long long total = q4_block_sum(units, sh_sum);
-  const long long target = (total + Q4_PIECES - 1) / Q4_PIECES;
+  const long long share = (((long long)total << sc.unit_shift) * p.Hkv + Q4_PIECES - 1) / Q4_PIECES;
+  const int per_piece = share < 1 ? 1 : share < (1 << 30) ? (int)share : 1 << 30;
   int base = 0, sbase = 0;
-  if (tid == 0) sh_found[0] = -1;
   for (int c = 0; c < rounds; ++c) {
     if (rounds > 1) load(c);
-    if (w == 0 && bad) flag_status(p.status, bad);         // (work-group 0 comes by every sequence before it finds its piece ...
-    const int pf = q4_pieces(sc, cut.blocks, cut.full ? Q4_ROWS : 0, target), pt = q4_pieces(sc, cut.blocks, cut.tail_rows, target);
-    const int pieces = p.Hkv * (cut.full * pf + pt);
-    const int split = p.Hkv * (cut.full * (pf > 1 ? pf : 0) + (pt > 1 ? pt : 0));
-    const int it = wave_incl_scan(pieces), st = wave_incl_scan(split);
-    __syncthreads();
-    if (lane == 63) { sh_w[wave][0] = it; sh_w[wave][1] = st; }
-    __syncthreads();
-    int b0 = base, s0 = sbase;
-    for (int q = 0; q < 4; ++q) {
-      if (q < wave) { b0 += sh_w[q][0]; s0 += sh_w[q][1]; }
-      base += sh_w[q][0]; sbase += sh_w[q][1];
+    const int pf = q4_pieces(sc, cut.blocks, cut.full ? Q4_ROWS : 0, per_piece), pt = q4_pieces(sc, cut.blocks, cut.tail_rows, per_piece);
+    const int per_head = cut.full * pf + pt, split_head = cut.full * (pf > 1 ? pf : 0) + (pt > 1 ? pt : 0);
+    const int it = wave_incl_scan(p.Hkv * per_head), st = wave_incl_scan(p.Hkv * split_head);
+    const int end = base + it, begin = end - p.Hkv * per_head;
+    const unsigned long long here = __ballot(w >= begin && w < end);
+    if (here) {
+      const int l = __ffsll((long long)here) - 1;
+      auto from = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+      int x = w - from(begin), sl = sbase + from(st - p.Hkv * split_head);
+      const int full = from(cut.full), f = from(pf), t = from(pt), ph = from(per_head);
+      out.head = x / ph;
+      x -= out.head * ph; sl += out.head * from(split_head);
+      if (x < full * f) { out.rt = x / f; x -= out.rt * f; out.pieces = f; sl += f > 1 ? out.rt * f : 0; }
+      else { out.rt = full; x -= full * f; out.pieces = t; sl += f > 1 ? full * f : 0; }
+      out.piece = x; out.slot = sl;
+      out.item = ((c * 64 + l) * p.Hkv + out.head) * sc.rt_max + out.rt;
+      out.s = SeqInfo{from(mine.L), from(mine.row0), from(mine.n), from(mine.k), from(mine.v), from(mine.nb), from(mine.page0), from(mine.npages)};
+      return true;
     }
-    const int begin = b0 + it - pieces;
-    if (w >= begin && w < begin + pieces) {
-      int x = w - begin, sl = s0 + st - split;
-      const int per_head = cut.full * pf + pt, split_head = cut.full * (pf > 1 ? pf : 0) + (pt > 1 ? pt : 0);
-      const int head = x / per_head;
-      x -= head * per_head; sl += head * split_head;
-      int rt, n;
-      if (x < cut.full * pf) { rt = x / pf; x -= rt * pf; n = pf; sl += pf > 1 ? rt * pf : 0; }
-      else { rt = cut.full; x -= cut.full * pf; n = pt; sl += pf > 1 ? cut.full * pf : 0; }
-      const int i = c * Q4_BLOCK + tid;
-      sh_found[0] = (i * p.Hkv + head) * sc.rt_max + rt; sh_found[1] = head; sh_found[2] = rt; sh_found[3] = x; sh_found[4] = n; sh_found[5] = sl;
-      sh_found[6] = mine.L; sh_found[7] = mine.row0; sh_found[8] = mine.n; sh_found[9] = mine.k; sh_found[10] = mine.v; sh_found[11] = mine.nb;
-      sh_found[12] = mine.page0; sh_found[13] = mine.npages;
-    }
-    if (w < base && w > 0) break;                          // (uniform; ... and by those behind it)
+    base += __builtin_amdgcn_readlane(it, 63);
+    sbase += __builtin_amdgcn_readlane(st, 63);
   }
-  __syncthreads();
-  auto found = [&](int k) { return __builtin_amdgcn_readfirstlane(sh_found[k]); };
-  out.item = found(0); out.head = found(1); out.rt = found(2); out.piece = found(3); out.pieces = found(4); out.slot = found(5);
-  out.s = SeqInfo{found(6), found(7), found(8), found(9), found(10), found(11), found(12), found(13)};
-  return out.item >= 0;
+  return false;
 }
 
 __device__ __forceinline__ bf16x8 as_bf16x8(u32x4 x) { return __builtin_bit_cast(bf16x8, x); }
@@ -146,6 +123,17 @@ __device__ __forceinline__ float max_halves(float x) {
 __device__ __forceinline__ float add_halves(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+typedef __attribute__((ext_vector_type(8))) int i32x8;
+// x += K Q^T over 64 channels: 32 codes of a key with their scale (byte BYTE of ks) and the two parts of the query.
+template <int BYTE>
+__device__ __forceinline__ f32x16 scores(u32x4 k, unsigned ks, i32x8 qh, i32x8 ql, int uh, int ul, f32x16 x) {
+  typedef __attribute__((ext_vector_type(4))) int i32x4;
+  const i32x4 k4 = __builtin_bit_cast(i32x4, k);
+  const i32x8 a = __builtin_shufflevector(k4, k4, 0, 1, 2, 3, -1, -1, -1, -1);
+  x = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, ql, x, 4, 0, BYTE, (int)ks, 0, ul);       // formats: 4 = e2m1, 0 = e4m3
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, qh, x, 4, 0, BYTE, (int)ks, 0, uh);
 }
 
 // Codes and scales of a block as a lane holds them.
@@ -229,17 +217,47 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
   const int ti = pc.rt * Q4_ROWS + (row_on ? tr : 0);
   const int nr = ti / p.G, g = ti - nr * p.G;            // new row, query head of the group
   const bf16_t* qrow = reinterpret_cast<const bf16_t*>(p.q) + ((long long)(s.row0 + nr) * p.Hq + pc.head * p.G + g) * DH;
-  u32x4 qf[STEPS];
+  u32x4 qw[4 * NA];                                      // channels 64 a + 16 h .. and 64 a + 32 + 16 h .., sixteen each
 #pragma unroll
-  for (int t = 0; t < STEPS; ++t) qf[t] = *reinterpret_cast<const u32x4*>(qrow + 64 * (t / 4) + 32 * h + 8 * (t % 4));
+  for (int t = 0; t < 4 * NA; ++t) qw[t] = *reinterpret_cast<const u32x4*>(qrow + 64 * (t / 4) + 32 * (t / 2 % 2) + 16 * h + 8 * (t % 2));
   if (count > 0) {
     request(ra, pa);
     if (count > 1) request(rb_, pb);
     pa = find_pages(2); pb = find_pages(3);
   }
+  // The query as the sum of two e4m3 numbers: q = 2^u hi + 2^(u-5) lo with 2^u hi up to 2^(u+8) the row's largest magnitude.  hi keeps four significant
+  // bits, what is left of a bf16's eight fits four more: exact for all but elements 2^-14 of the largest, and those to 2^-22 of it.
+  i32x8 qh[NA], ql[NA];
+  int uh, ul;                                            // exponents + 127, a byte
+  {
+    unsigned top = 0;
 #pragma unroll
-  for (int t = 0; t < STEPS; ++t)
-    if (!row_on) qf[t] = u32x4{0, 0, 0, 0};
+    for (int t = 0; t < 4 * NA; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) top = max(top, max(qw[t][e] & 0x7fff0000u, (qw[t][e] << 16) & 0x7fff0000u));
+    const auto both = __builtin_amdgcn_permlane32_swap(top, top, false, false);
+    top = max(both[0], both[1]);
+    const int b = clampi((int)(top >> 23) - 7, 6, 247);
+    uh = b; ul = top < 0x7f800000u ? b - 5 : 255;        // (a row with an infinity or a NaN: its scores are NaN)
+    const float up = __uint_as_float((unsigned)(254 - b) << 23);
+#pragma unroll
+    for (int a = 0; a < NA; ++a)
+#pragma unroll
+      for (int w = 0; w < 8; ++w) {                      // a word: four elements
+        const u32x4 x = qw[4 * a + w / 2];
+        const unsigned x0 = x[w % 2 * 2], x1 = x[w % 2 * 2 + 1];
+        const float f[4] = {__uint_as_float(x0 << 16) * up, __uint_as_float(x0 & 0xffff0000u) * up, __uint_as_float(x1 << 16) * up, __uint_as_float(x1 & 0xffff0000u) * up};
+        int hi = 0, lo = 0;
+        hi = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], hi, false);
+        hi = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], hi, true);
+        const f32x2 h0 = __builtin_amdgcn_cvt_pk_f32_fp8(hi, false), h1 = __builtin_amdgcn_cvt_pk_f32_fp8(hi, true);
+        lo = __builtin_amdgcn_cvt_pk_fp8_f32((f[0] - h0[0]) * 32.f, (f[1] - h0[1]) * 32.f, lo, false);
+        lo = __builtin_amdgcn_cvt_pk_fp8_f32((f[2] - h1[0]) * 32.f, (f[3] - h1[1]) * 32.f, lo, true);
+        qh[a][w] = row_on ? hi : 0;
+        ql[a][w] = row_on ? lo : 0;
+      }
+    if (!row_on) ul = 127;
+  }
   const float scale2 = p.sm_scale * 1.44269504088896340736f;
 
   f32x16 o[NC];
@@ -249,26 +267,35 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
     for (int e = 0; e < 16; ++e) o[cc][e] = 0.f;
   float m = -3e38f, l = 0.f;                             // running maximum (scaled, base 2) and sum
 
-  // scores -> probabilities; the running maximum and sum, and what O has to shrink by
+  // Scores -> probabilities.  They are taken against the running maximum as it stands; only where a row's sixteen sum to more than
+  // Q4_LAZY (the first block does) is the maximum found, and what was summed so far shrunk to it.  Sums and bf16 probabilities have the same
+  // relative precision whatever the reference, and a maximum costs as much as half the exponentials.
   auto softmax = [&](f32x16& x) {
-    float t[4];
+    f32x16 y;
+    auto exponentials = [&]() {
+      float t[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) t[e] = fmaxf(fmaxf(x[4 * e], x[4 * e + 1]), fmaxf(x[4 * e + 2], x[4 * e + 3]));
-    const float top = max_halves(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]))) * scale2;
-    if (__any(top > m + Q4_LAZY)) {
-      const float mn = fmaxf(m, top), f = __builtin_amdgcn_exp2f(m - mn);
+      for (int e = 0; e < 16; ++e) y[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], scale2, -m));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) t[e] = (y[4 * e] + y[4 * e + 1]) + (y[4 * e + 2] + y[4 * e + 3]);
+      return (t[0] + t[1]) + (t[2] + t[3]);
+    };
+    float sum = exponentials();
+    if (__any(sum > Q4_LAZY)) {
+      float top = x[0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) top = fmaxf(top, x[e]);
+      const float mn = fmaxf(m, max_halves(top) * scale2), f = __builtin_amdgcn_exp2f(m - mn);
       m = mn;
       l *= f;
 #pragma unroll
       for (int cc = 0; cc < NC; ++cc)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[cc][e] *= f;
+      sum = exponentials();
     }
-#pragma unroll
-    for (int e = 0; e < 16; ++e) x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], scale2, -m));
-#pragma unroll
-    for (int e = 0; e < 4; ++e) t[e] = (x[4 * e] + x[4 * e + 1]) + (x[4 * e + 2] + x[4 * e + 3]);
-    l += (t[0] + t[1]) + (t[2] + t[3]);
+    l += sum;
+    x = y;
   };
   // left: keys of the block, at least 32 unless MASKED
   auto multiply = [&](const Q4Regs<DH>& r, int left, auto masked) {
@@ -277,10 +304,7 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
 #pragma unroll
     for (int e = 0; e < 16; ++e) x[e] = 0.f;
 #pragma unroll
-    for (int t = 0; t < STEPS; ++t) {
-      const float ks = q4_key_scale((r.ks >> (8 * (2 * (t / 4) + h))) & 255u);
-      x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(q4_to_bf16(r.k[t / 4][t % 4], ks)), as_bf16x8(qf[t]), x, 0, 0, 0);
-    }
+    for (int a = 0; a < NA; ++a) x = a == 0 ? scores<0>(r.k[0], r.ks >> (8 * h), qh[0], ql[0], uh, ul, x) : scores<2>(r.k[NA - 1], r.ks >> (8 * h), qh[NA - 1], ql[NA - 1], uh, ul, x);
     if (MASKED) {
 #pragma unroll
       for (int e = 0; e < 16; ++e)
@@ -328,10 +352,17 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
   {
     int b = first > cached ? first : cached;             // the wave's first block at or behind `cached`
     b += (slot - (b - first)) & (KS - 1);
+    if (b < last) {
     const RowWindow win = row_window(nr, s);
     const long long stride = (long long)p.Hkv * DH;
     const bf16_t* k0 = reinterpret_cast<const bf16_t*>(p.k_new) + s.row0 * stride + (long long)pc.head * DH;
     const bf16_t* v0 = reinterpret_cast<const bf16_t*>(p.v_new) + s.row0 * stride + (long long)pc.head * DH;
+    u32x4 qf[STEPS];
+#pragma unroll
+    for (int t = 0; t < STEPS; ++t) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(qrow + 64 * (t / 4) + 32 * h + 8 * (t % 4));
+      qf[t] = row_on ? x : u32x4{0, 0, 0, 0};
+    }
     for (; b < last; b += KS) {
       const int t0 = 32 * (b - cached);
       const bf16_t* krow = k0 + min(t0 + key_of_row, s.n - 1) * stride;         // (behind the last row: that row, which the mask below leaves out)
@@ -394,6 +425,7 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
         }
         __builtin_amdgcn_wave_barrier();
       }
+    }
     }
   }
   l = add_halves(l);
@@ -512,7 +544,7 @@ __global__ __launch_bounds__(256) void attn_q4_combine_kernel(AttnParams p, Q4Sc
 }
 
 // Items of the largest sequence, partial slots and work-groups that there can be, and the workspace.
-struct Q4Shape { long long items, partials, wgs; int rt_max, fixed; size_t off_ml, off_entries, total; };
+struct Q4Shape { long long items, partials, wgs; int rt_max, fixed, unit_shift; size_t off_ml, off_entries, total; };
 static Q4Shape q4_shape(int batch, int num_kv_heads, int group, int total_rows, int max_kv_len, int max_new_rows, int kv_chunk, int head_dim) {
   Q4Shape z;
   const long long tile_rows = (long long)max_new_rows * group;
@@ -522,6 +554,10 @@ static Q4Shape q4_shape(int batch, int num_kv_heads, int group, int total_rows, 
   const long long seqs = batch < total_rows ? batch : total_rows;       // sequences that have rows
   z.items = seqs * num_kv_heads * z.rt_max;
   const long long blocks = ((long long)max_kv_len + Q4_TK - 1) / Q4_TK + (max_new_rows + Q4_TK - 1) / Q4_TK;
+  // units of all sequences' work: sequences whose rows add up to total_rows at most, every one as long as may be
+  const double units = ((double)total_rows * group / 32 + 2.0 * seqs) * 2 * (double)blocks;
+  z.unit_shift = 0;
+  while (units / (double)(1ll << z.unit_shift) >= 1073741824.0) ++z.unit_shift;
   if (z.fixed > 0) {
     z.wgs = z.items * ((blocks + z.fixed - 1) / z.fixed);
     z.partials = z.wgs;
@@ -550,7 +586,7 @@ size_t attn_q4_workspace(int batch, int num_kv_heads, int group, int total_rows,
 hipError_t run_attn_q4(const AttnParams& p, const Q4Cache& c, void* workspace, int kv_chunk, hipStream_t st) {
   const Q4Shape z = q4_shape(p.B, p.Hkv, p.G, p.total_rows, p.max_kv_len, p.max_new_rows, kv_chunk, p.D);
   char* ws = reinterpret_cast<char*>(workspace);
-  const Q4Sched sc = {z.fixed, z.rt_max, (int)z.partials, reinterpret_cast<float*>(ws), reinterpret_cast<float*>(ws + z.off_ml), reinterpret_cast<int2*>(ws + z.off_entries)};
+  const Q4Sched sc = {z.fixed, z.unit_shift, z.rt_max, (int)z.partials, reinterpret_cast<float*>(ws), reinterpret_cast<float*>(ws + z.off_ml), reinterpret_cast<int2*>(ws + z.off_entries)};
   if (z.wgs == 0) return hipSuccess;
   const int per_row = p.D / 8, most_rows = (int)((long long)p.max_new_rows * p.G < Q4_ROWS ? p.max_new_rows * p.G : Q4_ROWS);
   const dim3 grid((unsigned)((long long)p.B * p.Hkv * z.rt_max), (most_rows * per_row + 255) / 256);

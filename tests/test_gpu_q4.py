@@ -266,6 +266,34 @@ def test_a_stored_nan_is_seen_by_every_row_of_its_sequence(fd):
     n = int(call.row_indptr[1])
     assert np.isfinite(out[:n]).all() and np.isnan(out[n:, 0]).all() and np.isfinite(out[n:, 1]).all()
     assert np.isfinite(lse).all()
+    for group in range(4):                                # a NaN among 32 channels of a key
+        call.cache.v_scale[page, 0, 4] = 0.5
+        call.cache.k_scale[page, 0, 4] = 125
+        call.cache.k_scale[page, 0, 4, group] = 255
+        out, lse = call.upload().run()
+        assert np.isfinite(out[:n]).all() and np.isnan(out[n:, 0]).all() and np.isfinite(out[n:, 1]).all()
+        assert np.isnan(lse[n:, 0]).all() and np.isfinite(lse[n:, 1]).all() and np.isfinite(lse[:n]).all()
+
+
+def test_odd_queries_stay_in_their_row(fd):
+    """Queries of zeros, the smallest and the largest bf16s, infinities and NaN, and elements of very different size in one row."""
+    call = Q4Call(fd, kv=[300], k=[10], m=[0], hq=4, hkv=2, seed=7)
+    q = _wide(call.q)
+    q[0] = 0
+    q[1] *= 2.0 ** -125
+    q[2] *= 2.0 ** -100
+    q[3, :, ::2] *= 2.0 ** -20
+    q[4, :, 1:] *= 2.0 ** -13
+    q[5, :, :64] *= 2.0 ** -9
+    call.q = bits_of(q)
+    call.upload()
+    call.check(*call.run())
+    q[6, 1, 3], q[7, 0, 100], q[8, 2, 64] = np.inf, np.nan, -np.inf
+    call.q = bits_of(q)
+    out, lse = call.upload().run()
+    bad = np.zeros((10, 4), dtype=bool)
+    bad[6, 1] = bad[7, 0] = bad[8, 2] = True
+    assert np.isnan(out[bad]).all() and np.isfinite(out[~bad]).all() and np.isnan(lse[bad]).all() and np.isfinite(lse[~bad]).all()
 
 
 def test_rows_behind_the_last_sequence_stay(fd):
