@@ -110,6 +110,9 @@ __device__ __forceinline__ bool q4_find(const AttnParams& p, const Q4Sched& sc, 
   return false;
 }
 
+typedef __attribute__((ext_vector_type(8))) short s16x8;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
 __device__ __forceinline__ bf16x8 as_bf16x8(u32x4 x) { return __builtin_bit_cast(bf16x8, x); }
 __device__ __forceinline__ unsigned pack_bf16x2(float lo, float hi) {
   const f32x2 f = {lo, hi};
@@ -148,7 +151,7 @@ template <int DH>
 __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Cache c, Q4Sched sc) {
   constexpr int NA = DH / 64, NC = DH / 32, STEPS = DH / 16;
   constexpr int OP = DH + 4;                             // pitch of an O row in LDS, floats: an odd number of 16-byte slots
-  __shared__ float lds_o[4][32][OP];
+  __shared__ __align__(16) float lds_o[4][32][OP];
   __shared__ float lds_ml[4][32][2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l31 = lane & 31, h = lane >> 5;
@@ -348,67 +351,91 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
     if (t + 2 < count) multiply(ra, left(t + 2), ragged);
   }
 
-  // ---- the sequence's own rows, in bf16 ----
-  {
-    int b = first > cached ? first : cached;             // the wave's first block at or behind `cached`
-    b += (slot - (b - first)) & (KS - 1);
-    if (b < last) {
+  // ---- the sequence's own rows, in bf16: keys as the first operand straight from memory, values through this wave's part of LDS and its transposing read ----
+  int b = first > cached ? first : cached;               // the wave's first block at or behind `cached`
+  b += (slot - (b - first)) & (KS - 1);
+  if (b < last) {
+    constexpr int VP = DH + 32;                          // pitch of a row of values, bf16: the four rows of a transposing read use every bank once
+    static_assert(32 * VP * sizeof(bf16_t) <= sizeof(lds_o[0]), "a block of values fits a wave's part of LDS");
+    constexpr int LPR = DH / 8, RPL = 64 / LPR;          // lanes of a row, rows of a load
+    bf16_t* lv = reinterpret_cast<bf16_t*>(&lds_o[wave][0][0]);
     const RowWindow win = row_window(nr, s);
     const long long stride = (long long)p.Hkv * DH;
     const bf16_t* k0 = reinterpret_cast<const bf16_t*>(p.k_new) + s.row0 * stride + (long long)pc.head * DH;
     const bf16_t* v0 = reinterpret_cast<const bf16_t*>(p.v_new) + s.row0 * stride + (long long)pc.head * DH;
-    u32x4 qf[STEPS];
+    u32x4 qf[STEPS], kf[STEPS], vr[STEPS];
 #pragma unroll
-    for (int t = 0; t < STEPS; ++t) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(qrow + 64 * (t / 4) + 32 * h + 8 * (t % 4));
-      qf[t] = row_on ? x : u32x4{0, 0, 0, 0};
-    }
+    for (int t = 0; t < STEPS; ++t) qf[t] = *reinterpret_cast<const u32x4*>(qrow + 64 * (t / 4) + 32 * h + 8 * (t % 4));
+    // (behind the last row: that row, which the mask leaves out)
+    auto load_k = [&](int t0) {
+      const bf16_t* krow = k0 + min(t0 + key_of_row, s.n - 1) * stride;
+#pragma unroll
+      for (int t = 0; t < STEPS; ++t) kf[t] = *reinterpret_cast<const u32x4*>(krow + 64 * (t / 4) + 32 * h + 8 * (t % 4));
+    };
+    auto load_v = [&](int t0) {
+#pragma unroll
+      for (int t = 0; t < STEPS; ++t) vr[t] = *reinterpret_cast<const u32x4*>(v0 + min(t0 + RPL * t + lane / LPR, s.n - 1) * stride + lane % LPR * 8);
+    };
+    load_k(32 * (b - cached));
+    load_v(32 * (b - cached));
+#pragma unroll
+    for (int t = 0; t < STEPS; ++t)
+      if (!row_on) qf[t] = u32x4{0, 0, 0, 0};
     for (; b < last; b += KS) {
       const int t0 = 32 * (b - cached);
-      const bf16_t* krow = k0 + min(t0 + key_of_row, s.n - 1) * stride;         // (behind the last row: that row, which the mask below leaves out)
+      // A value that is no number must not reach a row that does not see it, and zero times it is NaN: it enters the product as zero.
+      unsigned odd = 0;                                  // (an exponent of all ones, plus one in its last place, reaches the sign)
+#pragma unroll
+      for (int t = 0; t < STEPS; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) odd |= (vr[t][e] & 0x7f807f80u) + 0x00800080u;
+      const bool any_odd = __any((odd & 0x80008000u) != 0);
+      if (any_odd) {
+#pragma unroll
+        for (int t = 0; t < STEPS; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if ((vr[t][e] & 0x7f80u) == 0x7f80u) vr[t][e] &= 0xffff0000u;
+            if ((vr[t][e] & 0x7f800000u) == 0x7f800000u) vr[t][e] &= 0xffffu;
+          }
+      }
+      __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+#pragma unroll
+      for (int t = 0; t < STEPS; ++t) *reinterpret_cast<u32x4*>(lv + (RPL * t + lane / LPR) * VP + lane % LPR * 8) = vr[t];
       f32x16 x;
 #pragma unroll
       for (int e = 0; e < 16; ++e) x[e] = 0.f;
 #pragma unroll
-      for (int t = 0; t < STEPS; ++t) {
-        const u32x4 kf = *reinterpret_cast<const u32x4*>(krow + 64 * (t / 4) + 32 * h + 8 * (t % 4));
-        x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kf), as_bf16x8(qf[t]), x, 0, 0, 0);
-      }
+      for (int t = 0; t < STEPS; ++t) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kf[t]), as_bf16x8(qf[t]), x, 0, 0, 0);
+      if (b + KS < last) { load_k(t0 + 32 * KS); load_v(t0 + 32 * KS); }
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const int t = t0 + 16 * (e / 8) + 8 * h + e % 8;
         x[e] = ((t < s.n) & new_key_visible(win, t)) ? x[e] : -INFINITY;
       }
       softmax(x);
-      // A value that is no number must not reach a row that does not see it, and zero times it is NaN: it enters the product as zero.
-      bool odd = false;
+      __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+      // (sixteen lanes read four keys of sixteen channels, and each gets its channel's four)
+      const bf16_t* vt = lv + (8 * h + ((lane & 15) >> 2)) * VP + (l31 & 16) + 4 * (lane & 3);
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
         u32x4 pf;
 #pragma unroll
         for (int e = 0; e < 4; ++e) pf[e] = pack_bf16x2(x[8 * q + 2 * e], x[8 * q + 2 * e + 1]);
-        const bf16_t* vt[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) vt[e] = v0 + min(t0 + 16 * q + 8 * h + e, s.n - 1) * stride + l31;
 #pragma unroll
         for (int cc = 0; cc < NC; ++cc) {
-          unsigned v[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            v[e] = vt[e][32 * cc];
-            const bool bad = (v[e] & 0x7f80u) == 0x7f80u;
-            odd |= bad;
-            v[e] = bad ? 0u : v[e];
-          }
-          const u32x4 vf = {v[0] | (v[1] << 16), v[2] | (v[3] << 16), v[4] | (v[5] << 16), v[6] | (v[7] << 16)};
-          o[cc] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vf), as_bf16x8(pf), o[cc], 0, 0, 0);
+          const s16x4 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + 16 * q * VP + 32 * cc));
+          const s16x4 w = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + (16 * q + 4) * VP + 32 * cc));
+          const s16x8 v = {u[0], u[1], u[2], u[3], w[0], w[1], w[2], w[3]};
+          o[cc] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), as_bf16x8(pf), o[cc], 0, 0, 0);
         }
       }
-      if (__any(odd)) {                                  // rare: infinities and NaN are added one by one where they are seen
-        float* mine = &lds_o[wave][l31][0];              // (this wave's part of LDS, free until the end; a row's 32 probabilities)
+      if (any_odd) {                                     // rare: infinities and NaN are added one by one where they are seen
+        float* mine = &lds_o[wave][l31][0];              // (a row's 32 probabilities, in place of the values)
+        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
 #pragma unroll
         for (int e = 0; e < 16; ++e) mine[16 * (e / 8) + 8 * h + e % 8] = x[e];
-        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
         const int n = min(32, s.n - t0);
 #pragma unroll 1
         for (int t = 0; t < n; ++t) {
@@ -423,10 +450,9 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
               if (!(fabsf(v) < INFINITY)) o[cc][a] += pr * v;
             }
         }
-        __builtin_amdgcn_wave_barrier();
       }
     }
-    }
+    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
   }
   l = add_halves(l);
 

@@ -1,0 +1,638 @@
+// Hybrid-mask verify+draft attention (Sec. 4.1) over a KV cache held in 4 bits, head dim 128 or 64.
+//
+// An item is one (sequence, KV head, up to 128 tile rows); a tile row is (new row, query head of the group).  Its keys,
+// cached ones and then the sequence's own new rows, form blocks of 32.  Items are cut into pieces of equal length, one per
+// work-group; an item of several pieces leaves (maximum, sum, un-normalised O) partials for the combine kernel.
+//
+// A wave takes 32 tile rows and a stream of blocks, by itself: with up to 32 tile rows the four waves of a work-group
+// take every fourth block, with up to 64 two waves a row block take every second, else each wave has its own rows and all blocks.
+// They meet once, when the piece ends and their (maximum, sum, O) are merged through LDS.  Nothing of the cache goes through LDS:
+//   S^T = K Q^T    v_mfma_f32_32x32x16_bf16.  A lane's eight channels of a key are one word of codes, so a lane loads its
+//                  half of a key's codes (sixteen bytes each 64 channels, one scale) and converts them in registers
+//   O^T += V^T P^T the layout of v_codes holds eight keys of a channel in one word for the same reason; the scale of a
+//                  value (one a token and head) is multiplied into P, which a lane holds for eight keys in a row
+// Which key a row of S^T stands for is free: row i = (b4 b3 b2 b1 b0) is key (b4 b2 b3 b1 b0), so that the sixteen scores that a lane holds
+// are two runs of eight keys, as the second product wants them.
+#include "kv_q4.h"
+#include <type_traits>
+
+namespace fd {
+
+constexpr int Q4_BLOCK = 256;
+constexpr int Q4_TK = 32;                 // keys of a block
+constexpr int Q4_ROWS = 128;              // tile rows of an item
+constexpr float Q4_LAZY = 256.f;          // sum of a row's sixteen probabilities from which on the softmax reference follows the row maximum
+constexpr int Q4_PIECES = 1024;           // pieces aimed at
+constexpr int Q4_MIN_PIECE = 8;           // blocks of a piece, at least (but for the last of a short item)
+
+struct Q4Sched {
+  int fixed;                // > 0: blocks of a piece, asked for by the caller
+  int unit_shift;           // work is counted in 2^unit_shift units
+  int rt_max;               // items of a (sequence, head), at most
+  int max_partials;         // partial slots in the workspace
+  float* part_acc;          // [max_partials][128][D] un-normalised O
+  float* part_ml;           // [max_partials][128][2] maximum (base 2), sum
+  int2* entries;            // [B * Hkv * rt_max]: pieces, first partial slot
+};
+
+// Row blocks that the waves of a work-group share out, for an item of so many tile rows.
+__device__ __forceinline__ int q4_row_blocks(int rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; }
+// How long a block takes a work-group, in halves: four waves take four blocks of one row block side by side, or one block of four.
+__device__ __forceinline__ int q4_weight(int rows) { return rows <= 32 ? 2 : rows <= 64 ? 3 : 6; }
+
+struct Q4Cut { int blocks, full, tail_rows; };          // of one sequence: blocks of its keys, items of 128 tile rows, rows of the last item
+__device__ __forceinline__ Q4Cut q4_cut(const AttnParams& p, const SeqInfo& s) {
+  Q4Cut c;
+  c.blocks = s.n > 0 ? (s.L + Q4_TK - 1) / Q4_TK + (s.n + Q4_TK - 1) / Q4_TK : 0;
+  const int rows = s.n * p.G;
+  c.full = rows / Q4_ROWS;
+  c.tail_rows = rows - c.full * Q4_ROWS;
+  return c;
+}
+// Pieces of an item of so many rows.  target: units of weight x blocks a piece should have.
+__device__ __forceinline__ int q4_pieces(const Q4Sched& sc, int blocks, int rows, int target) {
+  if (blocks <= 0 || rows <= 0) return 0;
+  const unsigned w = q4_weight(rows);
+  unsigned per = sc.fixed > 0 ? (unsigned)sc.fixed : ((unsigned)target + w - 1) / w;
+  if (sc.fixed <= 0 && per < Q4_MIN_PIECE) per = Q4_MIN_PIECE;
+  return (int)(((unsigned)blocks + per - 1) / per);
+}
+
+struct Q4Piece { int head, rt, piece, pieces, slot, item; SeqInfo s; };
+
+// Which piece work-group w takes: pieces are numbered by (sequence, head, item, piece).  Every wave finds it by itself, a sequence a lane, 64 at a
+// time: the lengths are one latency of memory, the rest lane shifts, and no wave waits for another.  false: none.
+__device__ __forceinline__ bool q4_find(const AttnParams& p, const Q4Sched& sc, int w, Q4Piece& out) {
+  const int lane = threadIdx.x & 63;
+  const int rounds = (p.B + 63) / 64;
+  Q4Cut cut = {};
+  SeqInfo mine = {};
+  auto load = [&](int c) {
+    cut = Q4Cut{};
+    uint32_t bad = 0;
+    const int i = c * 64 + lane;
+    if (i < p.B) { mine = load_seq_t<false>(p, i, &bad); cut = q4_cut(p, mine); }
+    if (bad && w == 0 && threadIdx.x < 64) flag_status(p.status, bad);        // (work-group 0 comes by every sequence)
+  };
+  int total = 0;                                         // units of weight x blocks of one head, in 2^unit_shift (the host's bounds say that they fit)
+  for (int c = 0; c < rounds; ++c) {
+    load(c);
+    const long long units = (long long)cut.blocks * (cut.full * q4_weight(Q4_ROWS) + (cut.tail_rows ? q4_weight(cut.tail_rows) : 0));
+    total += wave_total((int)((units + (1ll << sc.unit_shift) - 1) >> sc.unit_shift));      // (up, so that there are never more pieces than the host counts on)
+  }
+  const long long share = (((long long)total << sc.unit_shift) * p.Hkv + Q4_PIECES - 1) / Q4_PIECES;
+  const int per_piece = share < 1 ? 1 : share < (1 << 30) ? (int)share : 1 << 30;
+  int base = 0, sbase = 0;
+  for (int c = 0; c < rounds; ++c) {
+    if (rounds > 1) load(c);
+    const int pf = q4_pieces(sc, cut.blocks, cut.full ? Q4_ROWS : 0, per_piece), pt = q4_pieces(sc, cut.blocks, cut.tail_rows, per_piece);
+    const int per_head = cut.full * pf + pt, split_head = cut.full * (pf > 1 ? pf : 0) + (pt > 1 ? pt : 0);
+    const int it = wave_incl_scan(p.Hkv * per_head), st = wave_incl_scan(p.Hkv * split_head);
+    const int end = base + it, begin = end - p.Hkv * per_head;
+    const unsigned long long here = __ballot(w >= begin && w < end);
+    if (here) {
+      const int l = __ffsll((long long)here) - 1;
+      auto from = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+      int x = w - from(begin), sl = sbase + from(st - p.Hkv * split_head);
+      const int full = from(cut.full), f = from(pf), t = from(pt), ph = from(per_head);
+      out.head = x / ph;
+      x -= out.head * ph; sl += out.head * from(split_head);
+      if (x < full * f) { out.rt = x / f; x -= out.rt * f; out.pieces = f; sl += f > 1 ? out.rt * f : 0; }
+      else { out.rt = full; x -= full * f; out.pieces = t; sl += f > 1 ? full * f : 0; }
+      out.piece = x; out.slot = sl;
+      out.item = ((c * 64 + l) * p.Hkv + out.head) * sc.rt_max + out.rt;
+      out.s = SeqInfo{from(mine.L), from(mine.row0), from(mine.n), from(mine.k), from(mine.v), from(mine.nb), from(mine.page0), from(mine.npages)};
+      return true;
+    }
+    base += __builtin_amdgcn_readlane(it, 63);
+    sbase += __builtin_amdgcn_readlane(st, 63);
+  }
+  return false;
+}
+
+typedef __attribute__((ext_vector_type(8))) short s16x8;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+__device__ __forceinline__ bf16x8 as_bf16x8(u32x4 x) { return __builtin_bit_cast(bf16x8, x); }
+__device__ __forceinline__ unsigned pack_bf16x2(float lo, float hi) {
+  const f32x2 f = {lo, hi};
+  return __builtin_bit_cast(unsigned, __builtin_convertvector(f, bf16x2));      // round to nearest even
+}
+// The larger of a lane's value and that of lane ^ 32.
+__device__ __forceinline__ float max_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float add_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+typedef __attribute__((ext_vector_type(8))) int i32x8;
+// x += K Q^T over 64 channels: 32 codes of a key with their scale (byte BYTE of ks) and the two parts of the query.
+template <int BYTE>
+__device__ __forceinline__ f32x16 scores(u32x4 k, unsigned ks, i32x8 qh, i32x8 ql, int uh, int ul, f32x16 x) {
+  typedef __attribute__((ext_vector_type(4))) int i32x4;
+  const i32x4 k4 = __builtin_bit_cast(i32x4, k);
+  const i32x8 a = __builtin_shufflevector(k4, k4, 0, 1, 2, 3, -1, -1, -1, -1);
+  x = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, ql, x, 4, 0, BYTE, (int)ks, 0, ul);       // formats: 4 = e2m1, 0 = e4m3
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, qh, x, 4, 0, BYTE, (int)ks, 0, uh);
+}
+
+// Codes and scales of a block as a lane holds them.
+template <int DH> struct Q4Regs {
+  u32x4 k[DH / 64];          // its key's channels 64 a + 32 h ..: eight words of eight
+  unsigned ks;               // the key's scales, a byte each 32 channels
+  unsigned v[2][DH / 32];    // eight keys of channels 32 c + lane % 32, of either sixteen keys
+  u32x4 vs[2];               // the scales of those eight keys
+};
+
+template <int DH>
+__global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Cache c, Q4Sched sc) {
+  constexpr int NA = DH / 64, NC = DH / 32, STEPS = DH / 16;
+  constexpr int OP = DH + 4;                             // pitch of an O row in LDS, floats: an odd number of 16-byte slots
+  __shared__ __align__(16) float lds_o[4][32][OP];
+  __shared__ float lds_ml[4][32][2];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l31 = lane & 31, h = lane >> 5;
+  unsigned long long* STAMP = reinterpret_cast<unsigned long long*>(reinterpret_cast<char*>(sc.part_acc) + (256ll << 20)) + (long long)blockIdx.x * 8;
+  const unsigned long long T0 = wall_clock64();
+  Q4Piece pc;
+  if (!q4_find(p, sc, blockIdx.x, pc)) { if (threadIdx.x == 0) STAMP[0] = 0; return; }
+  const unsigned long long T1 = wall_clock64();
+  const SeqInfo& s = pc.s;
+  const int rows = min(Q4_ROWS, s.n * p.G - pc.rt * Q4_ROWS);
+  const int RB = q4_row_blocks(rows), ks_shift = RB == 1 ? 2 : RB == 2 ? 1 : 0, KS = 1 << ks_shift;
+  const int rb = wave & (RB - 1), slot = wave >> (2 - ks_shift);
+  const int cached = (s.L + Q4_TK - 1) / Q4_TK, blocks = cached + (s.n + Q4_TK - 1) / Q4_TK;
+  const int first = (int)((long long)blocks * pc.piece / pc.pieces), last = (int)((long long)blocks * (pc.piece + 1) / pc.pieces);
+
+  // ---- cached keys: which blocks, where they lie ----
+  const int lo = first + slot, hi = min(last, cached);
+  const int count = lo < hi ? (hi - lo + KS - 1) >> ks_shift : 0;        // blocks of this wave: lo, lo + KS, ...
+  // the pages of the wave's block t, sixteen keys each; past the last block, and for sixteen keys past the prefix, those of keys that are there
+  struct Pages { int page[2], slot[2]; };
+  auto find_pages = [&](int t) {
+    Pages r;
+    const int pos = 32 * (lo + (min(t, count - 1) << ks_shift));
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int x = q && pos + 16 < s.L ? pos + 16 : pos;
+      const int lp = (int)(__umulhi((unsigned)x, p.page_magic) >> p.page_magic_shift);
+      r.slot[q] = x - lp * p.page_size;
+      r.page[q] = sload(p.page_indices, s.page0 + lp);
+    }
+    return r;
+  };
+  auto token_of = [&](const Pages& r, int q) -> long long {
+    int page = r.page[q];
+    if (page < 0 || page >= p.num_pages) { if (lane == 0) flag_status(p.status, FD_DEV_PAGE_RANGE); page = 0; }
+    return q4_token(c, page, pc.head, p.page_size, r.slot[q]);
+  };
+  const int key_of_row = (l31 & 16) | ((l31 & 4) << 1) | ((l31 & 8) >> 1) | (l31 & 3);
+  auto request = [&](Q4Regs<DH>& r, const Pages& at) {
+    const long long w0 = token_of(at, 0), w1 = token_of(at, 1);
+    const long long mine = (key_of_row & 16 ? w1 : w0) + (key_of_row & 15);
+    const u32x4* k = reinterpret_cast<const u32x4*>(c.k_codes + mine * (DH / 2)) + h;
+#pragma unroll
+    for (int a = 0; a < NA; ++a) r.k[a] = k[2 * a];
+    if (DH == 128) r.ks = *reinterpret_cast<const unsigned*>(c.k_scales + mine * 4);
+    else r.ks = *reinterpret_cast<const unsigned short*>(c.k_scales + mine * 2);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const long long w = q ? w1 : w0;
+      const unsigned* v = reinterpret_cast<const unsigned*>(c.v_codes + w * (DH / 2)) + lane * NC;
+      if (DH == 128) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(v);
+#pragma unroll
+        for (int cc = 0; cc < NC; ++cc) r.v[q][cc] = x[cc];
+      } else {
+        const u32x2 x = *reinterpret_cast<const u32x2*>(v);
+        r.v[q][0] = x[0]; r.v[q][1] = x[1];
+      }
+      r.vs[q] = *reinterpret_cast<const u32x4*>(c.v_scales + w + 8 * h);
+    }
+  };
+  Q4Regs<DH> ra, rb_;
+  Pages pa = {}, pb = {};
+  if (count > 0) { pa = find_pages(0); pb = find_pages(1); }
+
+  // ---- this lane's row and its query, as the second operand of S^T = K Q^T ----
+  const int tr = rb * 32 + l31;
+  const bool row_on = tr < rows;
+  const int ti = pc.rt * Q4_ROWS + (row_on ? tr : 0);
+  const int nr = ti / p.G, g = ti - nr * p.G;            // new row, query head of the group
+  const bf16_t* qrow = reinterpret_cast<const bf16_t*>(p.q) + ((long long)(s.row0 + nr) * p.Hq + pc.head * p.G + g) * DH;
+  u32x4 qw[4 * NA];                                      // channels 64 a + 16 h .. and 64 a + 32 + 16 h .., sixteen each
+#pragma unroll
+  for (int t = 0; t < 4 * NA; ++t) qw[t] = *reinterpret_cast<const u32x4*>(qrow + 64 * (t / 4) + 32 * (t / 2 % 2) + 16 * h + 8 * (t % 2));
+  if (count > 0) {
+    request(ra, pa);
+    if (count > 1) request(rb_, pb);
+    pa = find_pages(2); pb = find_pages(3);
+  }
+  // The query as the sum of two e4m3 numbers: q = 2^u hi + 2^(u-5) lo with 2^u hi up to 2^(u+8) the row's largest magnitude.  hi keeps four significant
+  // bits, what is left of a bf16's eight fits four more: exact for all but elements 2^-14 of the largest, and those to 2^-22 of it.
+  i32x8 qh[NA], ql[NA];
+  int uh, ul;                                            // exponents + 127, a byte
+  {
+    unsigned top = 0;
+#pragma unroll
+    for (int t = 0; t < 4 * NA; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) top = max(top, max(qw[t][e] & 0x7fff0000u, (qw[t][e] << 16) & 0x7fff0000u));
+    const auto both = __builtin_amdgcn_permlane32_swap(top, top, false, false);
+    top = max(both[0], both[1]);
+    const int b = clampi((int)(top >> 23) - 7, 6, 247);
+    uh = b; ul = top < 0x7f800000u ? b - 5 : 255;        // (a row with an infinity or a NaN: its scores are NaN)
+    const float up = __uint_as_float((unsigned)(254 - b) << 23);
+#pragma unroll
+    for (int a = 0; a < NA; ++a)
+#pragma unroll
+      for (int w = 0; w < 8; ++w) {                      // a word: four elements
+        const u32x4 x = qw[4 * a + w / 2];
+        const unsigned x0 = x[w % 2 * 2], x1 = x[w % 2 * 2 + 1];
+        const float f[4] = {__uint_as_float(x0 << 16) * up, __uint_as_float(x0 & 0xffff0000u) * up, __uint_as_float(x1 << 16) * up, __uint_as_float(x1 & 0xffff0000u) * up};
+        int hi = 0, lo = 0;
+        hi = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], hi, false);
+        hi = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], hi, true);
+        const f32x2 h0 = __builtin_amdgcn_cvt_pk_f32_fp8(hi, false), h1 = __builtin_amdgcn_cvt_pk_f32_fp8(hi, true);
+        lo = __builtin_amdgcn_cvt_pk_fp8_f32((f[0] - h0[0]) * 32.f, (f[1] - h0[1]) * 32.f, lo, false);
+        lo = __builtin_amdgcn_cvt_pk_fp8_f32((f[2] - h1[0]) * 32.f, (f[3] - h1[1]) * 32.f, lo, true);
+        qh[a][w] = row_on ? hi : 0;
+        ql[a][w] = row_on ? lo : 0;
+      }
+    if (!row_on) ul = 127;
+  }
+  if (count > 0) asm volatile("s_waitcnt vmcnt(0)" :: "v"(ra.ks), "v"(qw[0]));
+  const unsigned long long T2 = wall_clock64();
+  const float scale2 = p.sm_scale * 1.44269504088896340736f;
+
+  f32x16 o[NC];
+#pragma unroll
+  for (int cc = 0; cc < NC; ++cc)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[cc][e] = 0.f;
+  float m = -3e38f, l = 0.f;                             // running maximum (scaled, base 2) and sum
+
+  // Scores -> probabilities.  They are taken against the running maximum as it stands; only where a row's sixteen sum to more than
+  // Q4_LAZY (the first block does) is the maximum found, and what was summed so far shrunk to it.  Sums and bf16 probabilities have the same
+  // relative precision whatever the reference, and a maximum costs as much as half the exponentials.
+  auto softmax = [&](f32x16& x) {
+    f32x16 y;
+    auto exponentials = [&]() {
+      float t[4];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) y[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], scale2, -m));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) t[e] = (y[4 * e] + y[4 * e + 1]) + (y[4 * e + 2] + y[4 * e + 3]);
+      return (t[0] + t[1]) + (t[2] + t[3]);
+    };
+    float sum = exponentials();
+    if (__any(sum > Q4_LAZY)) {
+      float top = x[0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) top = fmaxf(top, x[e]);
+      const float mn = fmaxf(m, max_halves(top) * scale2), f = __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= f;
+#pragma unroll
+      for (int cc = 0; cc < NC; ++cc)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[cc][e] *= f;
+      sum = exponentials();
+    }
+    l += sum;
+    x = y;
+  };
+  // left: keys of the block, at least 32 unless MASKED
+  auto multiply = [&](const Q4Regs<DH>& r, int left, auto masked) {
+    constexpr bool MASKED = decltype(masked)::value;
+    f32x16 x;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = 0.f;
+#pragma unroll
+    for (int a = 0; a < NA; ++a) x = a == 0 ? scores<0>(r.k[0], r.ks >> (8 * h), qh[0], ql[0], uh, ul, x) : scores<2>(r.k[NA - 1], r.ks >> (8 * h), qh[NA - 1], ql[NA - 1], uh, ul, x);
+    if (MASKED) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (16 * (e / 8) + 8 * h + e % 8 >= left) x[e] = -INFINITY;
+    }
+    softmax(x);
+    // P times the values' scales; a slot behind the prefix holds anything, NaN too
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      u32x4 pf;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float p0 = x[8 * q + 2 * e] * __uint_as_float(r.vs[q][e] << 16), p1 = x[8 * q + 2 * e + 1] * __uint_as_float(r.vs[q][e] & 0xffff0000u);
+        if (MASKED) {
+          if (16 * q + 8 * h + 2 * e >= left) p0 = 0.f;
+          if (16 * q + 8 * h + 2 * e + 1 >= left) p1 = 0.f;
+        }
+        pf[e] = pack_bf16x2(p0, p1);
+      }
+#pragma unroll
+      for (int cc = 0; cc < NC; ++cc)
+        o[cc] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(q4_to_bf16(r.v[q][cc], 1.f)), as_bf16x8(pf), o[cc], 0, 0, 0);
+    }
+  };
+  // Two blocks are held, a third and a fourth are looked up.  Only the last block can be ragged, so the loop, which leaves one to three, masks nothing.
+  if (count > 0) {
+    constexpr std::false_type whole; constexpr std::true_type ragged;
+    auto left = [&](int t) { return s.L - 32 * (lo + (t << ks_shift)); };
+    int t = 0;
+    for (; t + 3 < count; t += 2) {
+      multiply(ra, 32, whole);
+      request(ra, pa);
+      pa = find_pages(t + 4);
+      multiply(rb_, 32, whole);
+      request(rb_, pb);
+      pb = find_pages(t + 5);
+    }
+    multiply(ra, left(t), ragged);
+    if (t + 2 < count) request(ra, pa);
+    if (t + 1 < count) multiply(rb_, left(t + 1), ragged);
+    if (t + 2 < count) multiply(ra, left(t + 2), ragged);
+  }
+
+  // ---- the sequence's own rows, in bf16: keys as the first operand straight from memory, values through this wave's part of LDS and its transposing read ----
+  int b = first > cached ? first : cached;               // the wave's first block at or behind `cached`
+  b += (slot - (b - first)) & (KS - 1);
+  if (b < last) {
+    constexpr int VP = DH + 32;                          // pitch of a row of values, bf16: the four rows of a transposing read use every bank once
+    static_assert(32 * VP * sizeof(bf16_t) <= sizeof(lds_o[0]), "a block of values fits a wave's part of LDS");
+    constexpr int LPR = DH / 8, RPL = 64 / LPR;          // lanes of a row, rows of a load
+    bf16_t* lv = reinterpret_cast<bf16_t*>(&lds_o[wave][0][0]);
+    const RowWindow win = row_window(nr, s);
+    const long long stride = (long long)p.Hkv * DH;
+    const bf16_t* k0 = reinterpret_cast<const bf16_t*>(p.k_new) + s.row0 * stride + (long long)pc.head * DH;
+    const bf16_t* v0 = reinterpret_cast<const bf16_t*>(p.v_new) + s.row0 * stride + (long long)pc.head * DH;
+    u32x4 qf[STEPS], kf[STEPS], vr[STEPS];
+#pragma unroll
+    for (int t = 0; t < STEPS; ++t) qf[t] = *reinterpret_cast<const u32x4*>(qrow + 64 * (t / 4) + 32 * h + 8 * (t % 4));
+    // (behind the last row: that row, which the mask leaves out)
+    auto load_k = [&](int t0) {
+      const bf16_t* krow = k0 + min(t0 + key_of_row, s.n - 1) * stride;
+#pragma unroll
+      for (int t = 0; t < STEPS; ++t) kf[t] = *reinterpret_cast<const u32x4*>(krow + 64 * (t / 4) + 32 * h + 8 * (t % 4));
+    };
+    auto load_v = [&](int t0) {
+#pragma unroll
+      for (int t = 0; t < STEPS; ++t) vr[t] = *reinterpret_cast<const u32x4*>(v0 + min(t0 + RPL * t + lane / LPR, s.n - 1) * stride + lane % LPR * 8);
+    };
+    load_k(32 * (b - cached));
+    load_v(32 * (b - cached));
+#pragma unroll
+    for (int t = 0; t < STEPS; ++t)
+      if (!row_on) qf[t] = u32x4{0, 0, 0, 0};
+    for (; b < last; b += KS) {
+      const int t0 = 32 * (b - cached);
+      // A value that is no number must not reach a row that does not see it, and zero times it is NaN: it enters the product as zero.
+      unsigned odd = 0;                                  // (an exponent of all ones, plus one in its last place, reaches the sign)
+#pragma unroll
+      for (int t = 0; t < STEPS; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) odd |= (vr[t][e] & 0x7f807f80u) + 0x00800080u;
+      const bool any_odd = __any((odd & 0x80008000u) != 0);
+      if (any_odd) {
+#pragma unroll
+        for (int t = 0; t < STEPS; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if ((vr[t][e] & 0x7f80u) == 0x7f80u) vr[t][e] &= 0xffff0000u;
+            if ((vr[t][e] & 0x7f800000u) == 0x7f800000u) vr[t][e] &= 0xffffu;
+          }
+      }
+      __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+#pragma unroll
+      for (int t = 0; t < STEPS; ++t) *reinterpret_cast<u32x4*>(lv + (RPL * t + lane / LPR) * VP + lane % LPR * 8) = vr[t];
+      f32x16 x;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[e] = 0.f;
+#pragma unroll
+      for (int t = 0; t < STEPS; ++t) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kf[t]), as_bf16x8(qf[t]), x, 0, 0, 0);
+      if (b + KS < last) { load_k(t0 + 32 * KS); load_v(t0 + 32 * KS); }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int t = t0 + 16 * (e / 8) + 8 * h + e % 8;
+        x[e] = ((t < s.n) & new_key_visible(win, t)) ? x[e] : -INFINITY;
+      }
+      softmax(x);
+      __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+      // (sixteen lanes read four keys of sixteen channels, and each gets its channel's four)
+      const bf16_t* vt = lv + (8 * h + ((lane & 15) >> 2)) * VP + (l31 & 16) + 4 * (lane & 3);
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        u32x4 pf;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) pf[e] = pack_bf16x2(x[8 * q + 2 * e], x[8 * q + 2 * e + 1]);
+#pragma unroll
+        for (int cc = 0; cc < NC; ++cc) {
+          const s16x4 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + 16 * q * VP + 32 * cc));
+          const s16x4 w = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + (16 * q + 4) * VP + 32 * cc));
+          const s16x8 v = {u[0], u[1], u[2], u[3], w[0], w[1], w[2], w[3]};
+          o[cc] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), as_bf16x8(pf), o[cc], 0, 0, 0);
+        }
+      }
+      if (any_odd) {                                     // rare: infinities and NaN are added one by one where they are seen
+        float* mine = &lds_o[wave][l31][0];              // (a row's 32 probabilities, in place of the values)
+        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+#pragma unroll
+        for (int e = 0; e < 16; ++e) mine[16 * (e / 8) + 8 * h + e % 8] = x[e];
+        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+        const int n = min(32, s.n - t0);
+#pragma unroll 1
+        for (int t = 0; t < n; ++t) {
+          if (!new_key_visible(win, t0 + t)) continue;
+          const float pr = mine[t];
+          const bf16_t* vrow = v0 + (t0 + t) * stride + 4 * h;
+#pragma unroll
+          for (int cc = 0; cc < NC; ++cc)
+#pragma unroll
+            for (int a = 0; a < 16; ++a) {
+              const float v = bf16_to_f32(vrow[32 * cc + 8 * (a / 4) + a % 4]);
+              if (!(fabsf(v) < INFINITY)) o[cc][a] += pr * v;
+            }
+        }
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+  }
+  l = add_halves(l);
+  asm volatile("" :: "v"(o[0][0]), "v"(l));
+  const unsigned long long T4 = wall_clock64();
+
+  // ---- the waves' parts of a row meet: O^T columns become rows of LDS ----
+  if (h == 0) { lds_ml[wave][l31][0] = m; lds_ml[wave][l31][1] = l; }
+#pragma unroll
+  for (int cc = 0; cc < NC; ++cc)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const f32x4 x = {o[cc][4 * q], o[cc][4 * q + 1], o[cc][4 * q + 2], o[cc][4 * q + 3]};
+      *reinterpret_cast<f32x4*>(&lds_o[wave][l31][32 * cc + 8 * q + 4 * h]) = x;
+    }
+  __syncthreads();
+  if (threadIdx.x == 0 && pc.piece == 0) sc.entries[pc.item] = make_int2(pc.pieces, pc.slot);
+  constexpr int TPR = 8, CPT = DH / TPR;                 // threads of a row, channels of a thread
+  const int part = threadIdx.x % TPR;
+  for (int r = threadIdx.x / TPR; r < rows; r += Q4_BLOCK / TPR) {
+    const int b = r / 32, lr = r % 32;
+    float M = -3e38f;
+    for (int k = 0; k < KS; ++k) M = fmaxf(M, lds_ml[b + RB * k][lr][0]);
+    float acc[CPT], sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < CPT; ++e) acc[e] = 0.f;
+    for (int k = 0; k < KS; ++k) {
+      const int w = b + RB * k;
+      const float f = __builtin_amdgcn_exp2f(lds_ml[w][lr][0] - M);
+      sum += f * lds_ml[w][lr][1];
+#pragma unroll
+      for (int e = 0; e < CPT; e += 4) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(&lds_o[w][lr][part * CPT + e]);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) acc[e + u] += f * x[u];
+      }
+    }
+    if (pc.pieces > 1) {
+      if (pc.slot + pc.piece >= sc.max_partials) continue;           // (only where the device's rows contradict the host's bounds)
+      const long long at = (long long)(pc.slot + pc.piece) * Q4_ROWS + r;
+      float* dst = sc.part_acc + at * DH + part * CPT;
+#pragma unroll
+      for (int e = 0; e < CPT; e += 4) *reinterpret_cast<f32x4*>(dst + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
+      if (part == 0) *reinterpret_cast<float2*>(sc.part_ml + at * 2) = make_float2(M, sum);
+    } else {
+      const int t = pc.rt * Q4_ROWS + r, n = t / p.G;
+      const long long orow = (long long)(s.row0 + n) * p.Hq + pc.head * p.G + (t - n * p.G);
+      const float inv = 1.f / sum;
+      u32x4* dst = reinterpret_cast<u32x4*>(reinterpret_cast<bf16_t*>(p.out) + orow * DH + part * CPT);
+#pragma unroll
+      for (int e = 0; e < CPT; e += 8)
+        dst[e / 8] = u32x4{pack_bf16x2(acc[e] * inv, acc[e + 1] * inv), pack_bf16x2(acc[e + 2] * inv, acc[e + 3] * inv),
+                           pack_bf16x2(acc[e + 4] * inv, acc[e + 5] * inv), pack_bf16x2(acc[e + 6] * inv, acc[e + 7] * inv)};
+      if (part == 0 && p.lse) p.lse[orow] = (M + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
+    }
+  }
+  asm volatile("s_waitcnt vmcnt(0)");
+  if (threadIdx.x == 0) { STAMP[0] = T0; STAMP[1] = T1; STAMP[2] = T2; STAMP[3] = T3; STAMP[4] = T4; STAMP[5] = wall_clock64(); STAMP[6] = count; STAMP[7] = (rows << 16) | pc.pieces; }
+}
+
+// Merge of the partials of split items, by rows: a row is taken by TPR = DH / 8 lanes, eight channels each.  TPR pieces at a time: lane j
+// reads the maximum and sum of piece j, so that they are one latency, and the rows' values are requested four pieces at once.
+template <int DH>
+__global__ __launch_bounds__(256) void attn_q4_combine_kernel(AttnParams p, Q4Sched sc) {
+  constexpr int TPR = DH / 8, RPB = 256 / TPR, AT_ONCE = 4;
+  const int item = blockIdx.x, rt = item % sc.rt_max, head = item / sc.rt_max % p.Hkv, seq = item / sc.rt_max / p.Hkv;
+  const int2 e = sc.entries[item];
+  // (a sequence without new rows, or with fewer, has no such item: what stands in its entry is old)
+  const int r0 = sload(p.row_indptr, seq), r1 = sload(p.row_indptr, seq + 1);
+  const int row0 = clampi(r0, 0, p.total_rows), new_rows = min(clampi(r1 - r0, 0, p.max_new_rows), p.total_rows - row0);
+  const int rows = min(Q4_ROWS, new_rows * p.G - rt * Q4_ROWS);
+  const int pieces = __builtin_amdgcn_readfirstlane(e.x), slot = __builtin_amdgcn_readfirstlane(e.y);
+  const int r = blockIdx.y * RPB + threadIdx.x / TPR, part = threadIdx.x % TPR;
+  if ((int)blockIdx.y * RPB >= rows || pieces <= 1 || slot < 0 || (long long)slot + pieces > sc.max_partials) return;
+  const int rr = r < rows ? r : 0;                       // (every lane takes part in the exchanges)
+  float M = -3e38f, sum = 0.f, acc[8] = {};
+  for (int q0 = 0; q0 < pieces; q0 += TPR) {
+    const int n = min(TPR, pieces - q0);
+    const long long at = (long long)(slot + q0) * Q4_ROWS + rr;
+    float2 ml = make_float2(-3e38f, 0.f);
+    if (part < n) ml = *reinterpret_cast<const float2*>(sc.part_ml + (at + (long long)part * Q4_ROWS) * 2);
+    float top = ml.x;
+#pragma unroll
+    for (int d = 1; d < TPR; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+    const float mn = fmaxf(M, top), shrink = __builtin_amdgcn_exp2f(M - mn);
+    const float f = __builtin_amdgcn_exp2f(ml.x - mn);   // this lane's piece
+    float add = f * ml.y;
+#pragma unroll
+    for (int d = 1; d < TPR; d <<= 1) add += __shfl_xor(add, d);
+    M = mn;
+    sum = sum * shrink + add;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) acc[u] *= shrink;
+    const float* src = sc.part_acc + at * DH + part * 8;
+    for (int q = 0; q < n; q += AT_ONCE) {
+      f32x4 x[AT_ONCE][2];
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) {
+        const f32x4* y = reinterpret_cast<const f32x4*>(src + (long long)min(q + u, n - 1) * Q4_ROWS * DH);
+        x[u][0] = y[0]; x[u][1] = y[1];
+      }
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) {
+        if (q + u >= n) break;                           // (uniform; no zero times an infinity)
+        const float w = __shfl(f, (int)(threadIdx.x & 63) / TPR * TPR + q + u);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) { acc[v] += w * x[u][0][v]; acc[4 + v] += w * x[u][1][v]; }
+      }
+    }
+  }
+  if (r >= rows) return;
+  const int t = rt * Q4_ROWS + r, n = t / p.G;
+  const long long orow = (long long)(row0 + n) * p.Hq + head * p.G + (t - n * p.G);
+  const float inv = 1.f / sum;
+  u32x4 w;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) w[u] = pack_bf16x2(acc[2 * u] * inv, acc[2 * u + 1] * inv);
+  *reinterpret_cast<u32x4*>(reinterpret_cast<bf16_t*>(p.out) + orow * DH + part * 8) = w;
+  if (part == 0 && p.lse) p.lse[orow] = (M + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
+}
+
+// Items of the largest sequence, partial slots and work-groups that there can be, and the workspace.
+struct Q4Shape { long long items, partials, wgs; int rt_max, fixed, unit_shift; size_t off_ml, off_entries, total; };
+static Q4Shape q4_shape(int batch, int num_kv_heads, int group, int total_rows, int max_kv_len, int max_new_rows, int kv_chunk, int head_dim) {
+  Q4Shape z;
+  const long long tile_rows = (long long)max_new_rows * group;
+  z.rt_max = (int)((tile_rows + Q4_ROWS - 1) / Q4_ROWS);
+  if (z.rt_max < 1) z.rt_max = 1;
+  z.fixed = kv_chunk / Q4_TK;
+  const long long seqs = batch < total_rows ? batch : total_rows;       // sequences that have rows
+  z.items = seqs * num_kv_heads * z.rt_max;
+  const long long blocks = ((long long)max_kv_len + Q4_TK - 1) / Q4_TK + (max_new_rows + Q4_TK - 1) / Q4_TK;
+  // units of all sequences' work: sequences whose rows add up to total_rows at most, every one as long as may be
+  const double units = ((double)total_rows * group / 32 + 2.0 * seqs) * 2 * (double)blocks;
+  z.unit_shift = 0;
+  while (units / (double)(1ll << z.unit_shift) >= 1073741824.0) ++z.unit_shift;
+  if (z.fixed > 0) {
+    z.wgs = z.items * ((blocks + z.fixed - 1) / z.fixed);
+    z.partials = z.wgs;
+  } else {
+    // pieces - 1 of an item stay below its weight x blocks / target, which sum to Q4_PIECES over all items
+    z.wgs = z.items + Q4_PIECES;
+    z.partials = 2 * Q4_PIECES;                                         // an item in c >= 2 pieces: c <= 2 (c - 1)
+    const long long most = z.items * ((blocks + Q4_MIN_PIECE - 1) / Q4_MIN_PIECE);
+    if (most < z.wgs) z.wgs = most;
+    if (most < z.partials) z.partials = most;
+  }
+  auto round = [](size_t x) { return (x + 255) / 256 * 256; };
+  z.off_ml = round((size_t)z.partials * Q4_ROWS * head_dim * sizeof(float));
+  z.off_entries = z.off_ml + round((size_t)z.partials * Q4_ROWS * 2 * sizeof(float));
+  z.total = z.off_entries + round((size_t)(batch > 0 ? batch : 1) * num_kv_heads * z.rt_max * sizeof(int2));
+  return z;
+}
+
+// 0 where the call is too large for one launch.
+size_t attn_q4_workspace(int batch, int num_kv_heads, int group, int total_rows, int max_kv_len, int max_new_rows, int kv_chunk, int head_dim) {
+  const Q4Shape z = q4_shape(batch, num_kv_heads, group, total_rows, max_kv_len, max_new_rows, kv_chunk, head_dim);
+  if (z.wgs >= (1ll << 31) || (long long)batch * num_kv_heads * z.rt_max >= (1ll << 31)) return 0;
+  return z.total > 0 ? z.total : 256;
+}
+
+hipError_t run_attn_q4(const AttnParams& p, const Q4Cache& c, void* workspace, int kv_chunk, hipStream_t st) {
+  const Q4Shape z = q4_shape(p.B, p.Hkv, p.G, p.total_rows, p.max_kv_len, p.max_new_rows, kv_chunk, p.D);
+  char* ws = reinterpret_cast<char*>(workspace);
+  const Q4Sched sc = {z.fixed, z.unit_shift, z.rt_max, (int)z.partials, reinterpret_cast<float*>(ws), reinterpret_cast<float*>(ws + z.off_ml), reinterpret_cast<int2*>(ws + z.off_entries)};
+  if (z.wgs == 0) return hipSuccess;
+  const int per_row = p.D / 8, most_rows = (int)((long long)p.max_new_rows * p.G < Q4_ROWS ? p.max_new_rows * p.G : Q4_ROWS);
+  const dim3 grid((unsigned)((long long)p.B * p.Hkv * z.rt_max), (most_rows * per_row + 255) / 256);
+  if (p.D == 128) {
+    hipLaunchKernelGGL(attn_q4_kernel<128>, dim3((unsigned)z.wgs), dim3(Q4_BLOCK), 0, st, p, c, sc);
+    hipLaunchKernelGGL(attn_q4_combine_kernel<128>, grid, dim3(256), 0, st, p, sc);
+  } else {
+    hipLaunchKernelGGL(attn_q4_kernel<64>, dim3((unsigned)z.wgs), dim3(Q4_BLOCK), 0, st, p, c, sc);
+    hipLaunchKernelGGL(attn_q4_combine_kernel<64>, grid, dim3(256), 0, st, p, sc);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace fd
