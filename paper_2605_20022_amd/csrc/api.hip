@@ -531,6 +531,8 @@ static fd_status check_q4_cache(const fd_q4_cache* c, int head_dim, int page_siz
   if (num_kv_heads <= 0 || num_kv_heads > 65535) return fail(FD_ERR_INVALID_ARG, "num_kv_heads %d", num_kv_heads);
   if (c->stride_page < 0 || c->stride_head < 0 || c->stride_page >= (1ll << 31) || c->stride_head >= (1ll << 31))
     return fail(FD_ERR_INVALID_ARG, "cache strides must be in [0, 2^31) blocks");
+  if (c->stride_page * page_size >= (1ll << 31) || c->stride_head * page_size >= (1ll << 31))
+    return fail(FD_ERR_UNSUPPORTED, "cache strides of 2^31 tokens or more");
   if (!aligned16(c->k_codes) || !aligned16(c->v_codes) || !aligned16(c->v_scales) || (reinterpret_cast<uintptr_t>(c->k_scales) & 3))
     return fail(FD_ERR_INVALID_ARG, "k_codes, v_codes and v_scales must be 16-byte aligned, k_scales 4-byte aligned");
   return FD_OK;

@@ -140,11 +140,13 @@ __device__ __forceinline__ f32x16 scores(u32x4 k, unsigned ks, i32x8 qh, i32x8 q
 }
 
 // Codes and scales of a block as a lane holds them.
-template <int DH> struct Q4Regs {
-  u32x4 k[DH / 64];          // its key's channels 64 a + 32 h ..: eight words of eight
-  unsigned ks;               // the key's scales, a byte each 32 channels
-  unsigned v[2][DH / 32];    // eight keys of channels 32 c + lane % 32, of either sixteen keys
-  u32x4 vs[2];               // the scales of those eight keys
+template <int DH> struct Q4Keys {
+  u32x4 code[DH / 64];       // its key's channels 64 a + 32 h ..: 32 each
+  unsigned scale;            // the key's scales, a byte each 32 channels
+};
+template <int DH> struct Q4Values {
+  unsigned code[2][DH / 32]; // eight keys of channels 32 c + lane % 32, of either sixteen keys
+  u32x4 scale[2];            // the scales of those eight keys
 };
 
 template <int DH>
@@ -167,52 +169,67 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
   // ---- cached keys: which blocks, where they lie ----
   const int lo = first + slot, hi = min(last, cached);
   const int count = lo < hi ? (hi - lo + KS - 1) >> ks_shift : 0;        // blocks of this wave: lo, lo + KS, ...
-  // the pages of the wave's block t, sixteen keys each; past the last block, and for sixteen keys past the prefix, those of keys that are there
+  // The pages of the wave's block t, sixteen keys each; for what lies past the last block or the prefix, those of keys that are there.
   struct Pages { int page[2], slot[2]; };
   auto find_pages = [&](int t) {
     Pages r;
     const int pos = 32 * (lo + (min(t, count - 1) << ks_shift));
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      const int x = q && pos + 16 < s.L ? pos + 16 : pos;
+      const int x = q ? min(pos + 16, (s.L - 1) & ~15) : pos;
       const int lp = (int)(__umulhi((unsigned)x, p.page_magic) >> p.page_magic_shift);
       r.slot[q] = x - lp * p.page_size;
       r.page[q] = sload(p.page_indices, s.page0 + lp);
     }
     return r;
   };
-  auto token_of = [&](const Pages& r, int q) -> long long {
-    int page = r.page[q];
-    if (page < 0 || page >= p.num_pages) { if (lane == 0) flag_status(p.status, FD_DEV_PAGE_RANGE); page = 0; }
-    return q4_token(c, page, pc.head, p.page_size, r.slot[q]);
-  };
-  const int key_of_row = (l31 & 16) | ((l31 & 4) << 1) | ((l31 & 8) >> 1) | (l31 & 3);
-  auto request = [&](Q4Regs<DH>& r, const Pages& at) {
-    const long long w0 = token_of(at, 0), w1 = token_of(at, 1);
-    const long long mine = (key_of_row & 16 ? w1 : w0) + (key_of_row & 15);
-    const u32x4* k = reinterpret_cast<const u32x4*>(c.k_codes + mine * (DH / 2)) + h;
-#pragma unroll
-    for (int a = 0; a < NA; ++a) r.k[a] = k[2 * a];
-    if (DH == 128) r.ks = *reinterpret_cast<const unsigned*>(c.k_scales + mine * 4);
-    else r.ks = *reinterpret_cast<const unsigned short*>(c.k_scales + mine * 2);
+  // Where sixteen keys lie.  The host has seen to it that a page's and a head's tokens fit 31 bits, so a product of 32 bits by 32 is all it takes.
+  struct Tokens { unsigned long long at[2]; };
+  const unsigned page_tokens = (unsigned)c.sp * (unsigned)p.page_size;
+  const unsigned long long head_tokens = (unsigned long long)((unsigned)c.sh * (unsigned)p.page_size) * (unsigned)pc.head;
+  unsigned bad_page = 0;
+  auto tokens = [&](const Pages& r) {
+    Tokens t;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      const long long w = q ? w1 : w0;
-      const unsigned* v = reinterpret_cast<const unsigned*>(c.v_codes + w * (DH / 2)) + lane * NC;
-      if (DH == 128) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(v);
+      const bool bad = (unsigned)r.page[q] >= (unsigned)p.num_pages;
+      bad_page |= bad;
+      t.at[q] = (unsigned long long)(bad ? 0u : (unsigned)r.page[q]) * page_tokens + (head_tokens + (unsigned)r.slot[q]);
+    }
+    return t;
+  };
+  const int key_of_row = (l31 & 16) | ((l31 & 4) << 1) | ((l31 & 8) >> 1) | (l31 & 3);
+  const unsigned k_off = (key_of_row & 15) * (DH / 2) + h * 16, ks_off = (key_of_row & 15) * (DH / 32);
+  auto request_keys = [&](Q4Keys<DH>& r, const Tokens& at) {
+    const unsigned char* k0 = c.k_codes + at.at[0] * (DH / 2); const unsigned char* k1 = c.k_codes + at.at[1] * (DH / 2);
+    const unsigned char* k = (key_of_row & 16 ? k1 : k0) + k_off;
+    const unsigned char* s0 = c.k_scales + at.at[0] * (DH / 32); const unsigned char* s1 = c.k_scales + at.at[1] * (DH / 32);
+    const unsigned char* ks = (key_of_row & 16 ? s1 : s0) + ks_off;
 #pragma unroll
-        for (int cc = 0; cc < NC; ++cc) r.v[q][cc] = x[cc];
+    for (int a = 0; a < NA; ++a) r.code[a] = *reinterpret_cast<const u32x4*>(k + 32 * a);
+    if (DH == 128) r.scale = *reinterpret_cast<const unsigned*>(ks);
+    else r.scale = *reinterpret_cast<const unsigned short*>(ks);
+  };
+  auto request_values = [&](Q4Values<DH>& r, const Tokens& at) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const unsigned char* v = c.v_codes + at.at[q] * (DH / 2);
+      if (DH == 128) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(v + (unsigned)lane * 16u);
+#pragma unroll
+        for (int cc = 0; cc < NC; ++cc) r.code[q][cc] = x[cc];
       } else {
-        const u32x2 x = *reinterpret_cast<const u32x2*>(v);
-        r.v[q][0] = x[0]; r.v[q][1] = x[1];
+        const u32x2 x = *reinterpret_cast<const u32x2*>(v + (unsigned)lane * 8u);
+        r.code[q][0] = x[0]; r.code[q][1] = x[1];
       }
-      r.vs[q] = *reinterpret_cast<const u32x4*>(c.v_scales + w + 8 * h);
+      r.scale[q] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const unsigned char*>(c.v_scales) + at.at[q] * 2 + (unsigned)h * 16u);
     }
   };
-  Q4Regs<DH> ra, rb_;
-  Pages pa = {}, pb = {};
-  if (count > 0) { pa = find_pages(0); pb = find_pages(1); }
+  Q4Keys<DH> ka, kb;
+  Q4Values<DH> va, vb;
+  Pages pg = {};
+  Tokens tok = {};
+  if (count > 0) pg = find_pages(0);
 
   // ---- this lane's row and its query, as the second operand of S^T = K Q^T ----
   const int tr = rb * 32 + l31;
@@ -224,9 +241,14 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
 #pragma unroll
   for (int t = 0; t < 4 * NA; ++t) qw[t] = *reinterpret_cast<const u32x4*>(qrow + 64 * (t / 4) + 32 * (t / 2 % 2) + 16 * h + 8 * (t % 2));
   if (count > 0) {
-    request(ra, pa);
-    if (count > 1) request(rb_, pb);
-    pa = find_pages(2); pb = find_pages(3);
+    const Pages p1 = find_pages(1), p2 = find_pages(2);
+    tok = tokens(pg);
+    request_keys(ka, tok);
+    request_values(va, tok);
+    pg = p2;
+    tok = tokens(p1);
+    request_keys(kb, tok);
+    request_values(vb, tok);
   }
   // The query as the sum of two e4m3 numbers: q = 2^u hi + 2^(u-5) lo with 2^u hi up to 2^(u+8) the row's largest magnitude.  hi keeps four significant
   // bits, what is left of a bf16's eight fits four more: exact for all but elements 2^-14 of the largest, and those to 2^-22 of it.
@@ -300,55 +322,65 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
     l += sum;
     x = y;
   };
-  // left: keys of the block, at least 32 unless MASKED
-  auto multiply = [&](const Q4Regs<DH>& r, int left, auto masked) {
-    constexpr bool MASKED = decltype(masked)::value;
+  auto key_scores = [&](const Q4Keys<DH>& r) {
     f32x16 x;
 #pragma unroll
     for (int e = 0; e < 16; ++e) x[e] = 0.f;
-#pragma unroll
-    for (int a = 0; a < NA; ++a) x = a == 0 ? scores<0>(r.k[0], r.ks >> (8 * h), qh[0], ql[0], uh, ul, x) : scores<2>(r.k[NA - 1], r.ks >> (8 * h), qh[NA - 1], ql[NA - 1], uh, ul, x);
-    if (MASKED) {
+    const unsigned ks = r.scale >> (8 * h);
+    x = scores<0>(r.code[0], ks, qh[0], ql[0], uh, ul, x);
+    if (NA == 2) x = scores<2>(r.code[NA - 1], ks, qh[NA - 1], ql[NA - 1], uh, ul, x);
+    return x;
+  };
+  auto weigh_values = [&](f32x16 x, Q4Values<DH>& r, int left) {        // left: keys of the block, if below 32
+    if (left < 32) {                                     // a slot behind the prefix holds anything, a NaN as its scale too
+      asm volatile("");                                  // (a branch: as selects this would run for every block)
 #pragma unroll
       for (int e = 0; e < 16; ++e)
         if (16 * (e / 8) + 8 * h + e % 8 >= left) x[e] = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int key = 16 * (e / 4) + 8 * h + 2 * (e % 4);
+        const unsigned w = r.scale[e / 4][e % 4];
+        r.scale[e / 4][e % 4] = key >= left ? 0u : key + 1 >= left ? w & 0xffffu : w;
+      }
     }
     softmax(x);
-    // P times the values' scales; a slot behind the prefix holds anything, NaN too
+    u32x4 pf[2];                                         // P times the values' scales
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      u32x4 pf;
+    for (int q = 0; q < 2; ++q)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float p0 = x[8 * q + 2 * e] * __uint_as_float(r.vs[q][e] << 16), p1 = x[8 * q + 2 * e + 1] * __uint_as_float(r.vs[q][e] & 0xffff0000u);
-        if (MASKED) {
-          if (16 * q + 8 * h + 2 * e >= left) p0 = 0.f;
-          if (16 * q + 8 * h + 2 * e + 1 >= left) p1 = 0.f;
-        }
-        pf[e] = pack_bf16x2(p0, p1);
-      }
+      for (int e = 0; e < 4; ++e)
+        pf[q][e] = pack_bf16x2(x[8 * q + 2 * e] * __uint_as_float(r.scale[q][e] << 16), x[8 * q + 2 * e + 1] * __uint_as_float(r.scale[q][e] & 0xffff0000u));
+    // codes are converted one product ahead, so that the matrix pipe does not wait for them
+    u32x4 vf[2];
+    vf[0] = q4_to_bf16(r.code[0][0], 1.f);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int cc = 0; cc < NC; ++cc)
-        o[cc] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(q4_to_bf16(r.v[q][cc], 1.f)), as_bf16x8(pf), o[cc], 0, 0, 0);
+    for (int i = 0; i < 2 * NC; ++i) {
+      if (i + 1 < 2 * NC) vf[(i + 1) & 1] = q4_to_bf16(r.code[(i + 1) / NC][(i + 1) % NC], 1.f);
+      o[i % NC] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vf[i & 1]), as_bf16x8(pf[i / NC]), o[i % NC], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
-  // Two blocks are held, a third and a fourth are looked up.  Only the last block can be ragged, so the loop, which leaves one to three, masks nothing.
+  // Keys and values of two blocks are held or on their way, the pages of a third are looked up.  Past the end the last block is requested again (its
+  // lines are at hand), so that nothing in the loop depends on the count; with an odd count the last step's second half weighs nothing.
   if (count > 0) {
-    constexpr std::false_type whole; constexpr std::true_type ragged;
-    auto left = [&](int t) { return s.L - 32 * (lo + (t << ks_shift)); };
-    int t = 0;
-    for (; t + 3 < count; t += 2) {
-      multiply(ra, 32, whole);
-      request(ra, pa);
-      pa = find_pages(t + 4);
-      multiply(rb_, 32, whole);
-      request(rb_, pb);
-      pb = find_pages(t + 5);
+    const int left0 = s.L - 32 * lo, step = 32 << ks_shift;
+    for (int t = 0; t < count; t += 2) {
+      f32x16 x = key_scores(ka);
+      tok = tokens(pg);
+      pg = find_pages(t + 3);
+      request_keys(ka, tok);
+      weigh_values(x, va, left0 - t * step);
+      request_values(va, tok);
+      x = key_scores(kb);
+      tok = tokens(pg);
+      pg = find_pages(t + 4);
+      request_keys(kb, tok);
+      weigh_values(x, vb, t + 1 < count ? left0 - (t + 1) * step : 0);
+      request_values(vb, tok);
     }
-    multiply(ra, left(t), ragged);
-    if (t + 2 < count) request(ra, pa);
-    if (t + 1 < count) multiply(rb_, left(t + 1), ragged);
-    if (t + 2 < count) multiply(ra, left(t + 2), ragged);
+    if (bad_page && lane == 0) flag_status(p.status, FD_DEV_PAGE_RANGE);
   }
 
   // ---- the sequence's own rows, in bf16: keys as the first operand straight from memory, values through this wave's part of LDS and its transposing read ----
