@@ -1,32 +1,45 @@
 // The 4-bit KV cache: commit of verified rows and read-back.
 //
-// Commit.  A work-group takes up to 64 tokens of one sequence and head, from a multiple of 16 slots on, so that no two
-// work-groups share a byte of v_codes (two tokens a byte).  A thread has 32 channels of one token: of the key it finds the
-// shared power of two and writes sixteen bytes of codes; of the value it finds the largest magnitude, which four
-// lanes combine to the token's scale, and leaves the values in LDS, from where they are taken eight tokens at a time.
-//
-// Read-back.  A work-group writes 64 rows of one head: keys by (token, 32 channels), values by (eight tokens, four
-// channels), the units in which the codes lie.
+// Both take 64 tokens of one sequence and head per work-group, from a multiple of eight (read-back) or sixteen (commit: two tokens share a byte
+// of v_codes, and no two work-groups may write one byte) slots on.  Sixteen lanes (eight at head dim 64) have a token, eight channels each: the
+// rows are read and written whole, and a key's power of two and a value's scale are maxima over four of them, and all.  Values
+// change between rows and the eight tokens to a word of v_codes in LDS.  Bound by HBM where there is much to do (rows 2 or 4 bytes
+// an element, codes a half), else by the latencies of lengths, page and row, one after the other.
 #include "kv_q4.h"
 
 namespace fd {
 
 constexpr int AQ_TOKENS = 64;
 
-__device__ __forceinline__ unsigned abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+// Largest of a value over 4 or N lanes in a row of sixteen, by lane shifts.
+template <int N>
+__device__ __forceinline__ unsigned max_over(unsigned v) {
+  v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0xb1, 0xf, 0xf, false));            // quad_perm 1 0 3 2
+  v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, false));            // quad_perm 2 3 0 1
+  if (N >= 8) v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, false));      // mirror in eight
+  if (N >= 16) v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xf, 0xf, false));     // mirror in sixteen
+  return v;
+}
+__device__ __forceinline__ unsigned top_of(u32x4 w) {      // largest magnitude of eight bf16, as the bits of an fp32: in order, and a NaN above every number
+  unsigned t = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) t = max(t, max(w[e] & 0x7fff0000u, (w[e] << 16) & 0x7fff0000u));
+  return t;
+}
 
 template <int DH>
 __global__ __launch_bounds__(256) void append_kv_q4_kernel(AttnParams p, Q4Cache c, const int* __restrict__ accept_len, int* kv_len_out) {
-  constexpr int GR = DH / 32;                        // channel groups of a token
-  constexpr int PITCH = DH + 2;                      // LDS row in bf16: an odd number of words
-  __shared__ bf16_t vals[AQ_TOKENS][PITCH];
-  __shared__ float scales[AQ_TOKENS];
+  constexpr int LPT = DH / 8, GR = DH / 32;          // lanes of a token, channel groups
+  constexpr int PITCH = DH + 8;                      // LDS row in bf16: rows stay 16-byte aligned
+  __shared__ __align__(16) bf16_t vals[AQ_TOKENS][PITCH];
+  __shared__ float2 inv[AQ_TOKENS];                  // a value is divided by its scale as (v x) y
   const int seq = blockIdx.x, head = blockIdx.y, tid = threadIdx.x;
+  const int accepted = sload(accept_len, seq);       // (requested with the lengths)
   const SeqInfo s = load_seq(p, seq);
   int rows = 0;
   const bool first = head == 0 && blockIdx.z == 0 && tid == 0;
   if (s.k > 0) {
-    int acc = accept_len[seq];
+    int acc = accepted;
     if (acc < 0 || acc >= s.k) { if (first) flag_status(p.status, FD_DEV_ROWS_RANGE); acc = clampi(acc, 0, s.k - 1); }
     rows = acc + 1;
     const long long room = (long long)s.npages * p.page_size - s.L;
@@ -38,58 +51,46 @@ __global__ __launch_bounds__(256) void append_kv_q4_kernel(AttnParams p, Q4Cache
   if (lo >= hi) return;
   // where a position lies; < 0: nowhere
   auto token_at = [&](int pos) -> long long {
-    const int lp = pos / p.page_size;
+    const int lp = (int)(__umulhi((unsigned)pos, p.page_magic) >> p.page_magic_shift);
     const int page = p.page_indices[s.page0 + lp];
     if (page < 0 || page >= p.num_pages) { if (head == 0) flag_status(p.status, FD_DEV_PAGE_RANGE); return -1; }
     return q4_token(c, page, head, p.page_size, pos - lp * p.page_size);
   };
-  {
-    const int t = tid / GR, g = tid % GR, pos = t0 + t;
-    if (t < AQ_TOKENS && pos >= lo && pos < hi) {
-      const long long row = ((long long)(s.row0 + pos - s.L) * p.Hkv + head) * DH + g * 32;
-      const long long at = token_at(pos);
-      u32x4 kw[4], vw[4];
+  const int g = tid % LPT;                           // channels 8 g ..
+  constexpr int PASSES = AQ_TOKENS * LPT / 256;
+  u32x4 kw[PASSES], vw[PASSES];
+  long long at[PASSES];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        kw[j] = reinterpret_cast<const u32x4*>(reinterpret_cast<const bf16_t*>(p.k_new) + row)[j];
-        vw[j] = reinterpret_cast<const u32x4*>(reinterpret_cast<const bf16_t*>(p.v_new) + row)[j];
+  for (int u = 0; u < PASSES; ++u) {                 // all rows are requested, with their pages, before the first is looked at
+    const int pos = t0 + u * (256 / LPT) + tid / LPT;
+    const bool on = pos >= lo && pos < hi;
+    const long long row = ((long long)(s.row0 + (on ? pos : lo) - s.L) * p.Hkv + head) * DH + g * 8;
+    at[u] = on ? token_at(pos) : -1;
+    kw[u] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const bf16_t*>(p.k_new) + row);
+    vw[u] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const bf16_t*>(p.v_new) + row);
+  }
+#pragma unroll
+  for (int u = 0; u < PASSES; ++u) {
+    const int t = u * (256 / LPT) + tid / LPT;
+    const unsigned ktop = max_over<4>(top_of(kw[u])), vtop = max_over<LPT>(top_of(vw[u]));
+    const bool kfinite = ktop < 0x7f800000u, vfinite = vtop < 0x7f800000u;
+    const int kb = q4_key_exponent(__uint_as_float(ktop));
+    const bf16_t vs = vfinite ? f32_to_bf16(__uint_as_float(vtop) / 6.f) : (bf16_t)0x7fc0;
+    if (at[u] >= 0) {
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[2 * e] = ldexpf(__uint_as_float(kw[u][e] << 16), 127 - kb);
+        x[2 * e + 1] = ldexpf(__uint_as_float(kw[u][e] & 0xffff0000u), 127 - kb);
       }
-      // magnitudes as integers: in order, and a NaN above every number
-      unsigned ktop = 0, vtop = 0;
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          ktop = max(ktop, max(kw[j][e] & 0x7fff0000u, (kw[j][e] << 16) & 0x7fff0000u));
-          vtop = max(vtop, max(vw[j][e] & 0x7fff0000u, (vw[j][e] << 16) & 0x7fff0000u));
-        }
-#pragma unroll
-      for (int d = 1; d < GR; d <<= 1) vtop = max(vtop, (unsigned)__shfl_xor((int)vtop, d));
-      const bool kfinite = ktop < 0x7f800000u, vfinite = vtop < 0x7f800000u;
-      const int kb = q4_key_exponent(__uint_as_float(ktop));
-      const bf16_t vs = vfinite ? f32_to_bf16(__uint_as_float(vtop) / 6.f) : (bf16_t)0x7fc0;
-      if (at >= 0) {
-        u32x4 codes;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float x[8];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            x[2 * e] = ldexpf(__uint_as_float(kw[j][e] << 16), 127 - kb);
-            x[2 * e + 1] = ldexpf(__uint_as_float(kw[j][e] & 0xffff0000u), 127 - kb);
-          }
-          codes[j] = kfinite ? f32_to_q4(x) : 0u;
-        }
-        *reinterpret_cast<u32x4*>(c.k_codes + at * (DH / 2) + g * 16) = codes;
-        c.k_scales[at * GR + g] = kfinite ? (unsigned char)kb : (unsigned char)255;
-        if (g == 0) c.v_scales[at] = vs;
-      }
-      unsigned* dst = reinterpret_cast<unsigned*>(&vals[t][g * 32]);
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) dst[4 * j + e] = vw[j][e];
-      if (g == 0) scales[t] = bf16_to_f32(vs);
+      *reinterpret_cast<unsigned*>(c.k_codes + at[u] * (DH / 2) + g * 4) = kfinite ? f32_to_q4(x) : 0u;
+      if (g % 4 == 0) c.k_scales[at[u] * GR + g / 4] = kfinite ? (unsigned char)kb : (unsigned char)255;
+      if (g == 0) c.v_scales[at[u]] = vs;
+    }
+    *reinterpret_cast<u32x4*>(&vals[t][g * 8]) = vfinite ? vw[u] : u32x4{0, 0, 0, 0};
+    if (g == 0) {
+      const float sc = bf16_to_f32(vs), pre = sc < 0x1p-100f ? 0x1p60f : 1.f;       // (the reciprocal of the smallest scales is no number)
+      inv[t] = make_float2(pre, vfinite && sc > 0.f ? 1.f / (sc * pre) : 0.f);
     }
   }
   __syncthreads();
@@ -97,29 +98,31 @@ __global__ __launch_bounds__(256) void append_kv_q4_kernel(AttnParams p, Q4Cache
     // eight tokens, channels 32 cc + j
     const int u = tid / 32, j = tid % 32, base = t0 + 8 * u;
     if (base < hi && base + 8 > lo) {
-      const long long at = token_at(base);
-      if (at >= 0) {
-        unsigned* dst = reinterpret_cast<unsigned*>(c.v_codes + (at / 16 * 16) * (DH / 2) + ((at / 8 & 1) * 32 + j) * GR * 4);
+      const long long tok = token_at(base);
+      if (tok >= 0) {
+        unsigned* dst = reinterpret_cast<unsigned*>(c.v_codes + (tok & ~15ll) * (DH / 2) + ((tok >> 3 & 1) * 32 + j) * GR * 4);
         unsigned keep = 0;                           // nibbles of tokens that are not written here
 #pragma unroll
         for (int e = 0; e < 8; ++e)
           if (base + e < lo || base + e >= hi) keep |= 15u << (4 * e);
+        unsigned old[GR];
+#pragma unroll
+        for (int cc = 0; cc < GR; ++cc) old[cc] = keep ? dst[cc] : 0u;
 #pragma unroll
         for (int cc = 0; cc < GR; ++cc) {
           float x[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const int t = 8 * u + e;
-            x[e] = 0.f;
-            if (base + e >= lo && base + e < hi) {
-              const float v = bf16_to_f32(vals[t][32 * cc + j]), sc = scales[t];
-              // (a correctly rounded quotient is a tie only where the exact one is: value and scale have 8 bits each)
-              x[e] = sc > 0.f ? v / sc : sc == 0.f ? copysignf(0.f, v) : 0.f;
-            }
+            const float2 d = inv[8 * u + e];         // (of tokens that are not written: any)
+            // Value and scale have eight bits each, so that a quotient that is not a midpoint between two codes is 2^-14 of it away: rounded to
+            // sixteen bits, the product with the reciprocal (2^-22) is the midpoint where the quotient is, and on its side of it where it is not.
+            const float y = bf16_to_f32(vals[8 * u + e][32 * cc + j]) * d.x * d.y;
+            x[e] = __uint_as_float((__float_as_uint(y) + 0x80u) & 0xffffff00u);
           }
-          const unsigned w = f32_to_q4(x);
-          dst[cc] = keep ? (dst[cc] & keep) | (w & ~keep) : w;
+          old[cc] = (old[cc] & keep) | (f32_to_q4(x) & ~keep);
         }
+        if (GR == 4) *reinterpret_cast<u32x4*>(dst) = u32x4{old[0], old[1], old[GR - 2], old[GR - 1]};
+        else *reinterpret_cast<u32x2*>(dst) = u32x2{old[0], old[1]};
       }
     }
   }
@@ -158,80 +161,113 @@ struct ReadParams {
   uint32_t* status;
 };
 
+// Eight values to a row.
+__device__ __forceinline__ void store8(float* dst, const float (&x)[8]) {
+  *reinterpret_cast<f32x4*>(dst) = f32x4{x[0], x[1], x[2], x[3]};
+  *reinterpret_cast<f32x4*>(dst + 4) = f32x4{x[4], x[5], x[6], x[7]};
+}
+__device__ __forceinline__ void store8(bf16_t* dst, const float (&x)[8]) {
+  u32x4 w;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) w[e] = (unsigned)f32_to_bf16(x[2 * e]) | ((unsigned)f32_to_bf16(x[2 * e + 1]) << 16);
+  *reinterpret_cast<u32x4*>(dst) = w;
+}
+
 template <int DH, typename T>
 __global__ __launch_bounds__(256) void read_kv_q4_kernel(ReadParams p, Q4Cache c, T* __restrict__ k_out, T* __restrict__ v_out) {
-  constexpr int GR = DH / 32;
+  constexpr int LPT = DH / 8, GR = DH / 32;
+  __shared__ __align__(16) unsigned vcodes[AQ_TOKENS / 8][32 * GR];
+  __shared__ long long where[AQ_TOKENS];               // of each token; < 0: nowhere
+  __shared__ float vscale[AQ_TOKENS];
   const int head = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
-  const int a = blockIdx.x * AQ_TOKENS, b = min(a + AQ_TOKENS, p.total_rows);
-  // the last sequence that starts at or before row a
-  int seq = -1;
-  for (int i0 = 0; i0 < p.B; i0 += 64) {
-    const unsigned long long at = __ballot(i0 + lane < p.B && p.out_indptr[i0 + lane] <= a);
-    if (at) seq = i0 + 63 - __clzll((long long)at);
-    if (at != ~0ull) break;
+  // Which 64 tokens: those of a sequence are counted from a multiple of eight on.  Every wave finds it by itself, a sequence a lane.
+  int seq = -1, o0 = 0, n = 0, s0 = 0, chunk = 0;
+  for (int c0 = 0, base = 0; c0 < p.B; c0 += 64) {
+    const int i = c0 + lane;
+    int a = 0, rows = 0, st = 0, chunks = 0;
+    if (i < p.B) {
+      a = clampi(p.out_indptr[i], 0, p.total_rows);
+      rows = clampi(p.out_indptr[i + 1], 0, p.total_rows) - a;
+      st = p.start ? p.start[i] : 0;
+      if (rows > 0) chunks = ((st & 7) + rows + AQ_TOKENS - 1) / AQ_TOKENS;
+    }
+    const int incl = base + wave_incl_scan(chunks);
+    const unsigned long long here = __ballot((int)blockIdx.x >= incl - chunks && (int)blockIdx.x < incl);
+    if (here) {
+      const int l = __ffsll((long long)here) - 1;
+      auto from = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+      seq = c0 + l; o0 = from(a); n = from(rows); s0 = from(st); chunk = blockIdx.x - from(incl - chunks);
+      break;
+    }
+    base = __builtin_amdgcn_readlane(incl, 63);
   }
-  bool bad = false;
-  for (seq = seq < 0 ? 0 : seq; seq < p.B; ++seq) {
-    const int o0 = clampi(p.out_indptr[seq], 0, p.total_rows), o1 = clampi(p.out_indptr[seq + 1], 0, p.total_rows);
-    if (o0 >= b) break;
-    const int r0 = max(a, o0), r1 = min(b, o1);                    // rows of this sequence in this work-group
-    if (r0 >= r1) continue;
-    const int s0 = p.start ? p.start[seq] : 0;
-    const int pg0 = clampi(p.page_indptr[seq], 0, p.page_entries), pg1 = clampi(p.page_indptr[seq + 1], pg0, p.page_entries);
-    const long long room = (long long)(pg1 - pg0) * p.page_size;
-    const long long first = (long long)s0 + (r0 - o0);             // position of row r0
-    auto token_at = [&](long long pos) -> long long {
-      if (pos < 0 || pos >= room) { bad = true; return -1; }
+  if (seq < 0) return;
+  const int pg0 = clampi(sload(p.page_indptr, seq), 0, p.page_entries), pg1 = clampi(sload(p.page_indptr, seq + 1), pg0, p.page_entries);
+  const long long room = (long long)(pg1 - pg0) * p.page_size;
+  const long long first = (long long)s0 - (s0 & 7) + (long long)chunk * AQ_TOKENS;           // position of token 0 of this work-group
+  const long long shift = first - s0;                  // token t is row o0 + shift + t, where that is one of the n
+  if (tid < AQ_TOKENS) {
+    const long long pos = first + tid;
+    const bool asked = shift + tid >= 0 && shift + tid < n;
+    long long at = -1;
+    bool bad = false;
+    if (pos >= 0 && pos < room) {
       const int lp = (int)((unsigned)pos / (unsigned)p.page_size);
       const int page = p.page_indices[pg0 + lp];
-      if (page < 0 || page >= p.num_pages) { bad = true; return -1; }
-      return q4_token(c, page, head, p.page_size, (int)((unsigned)pos - (unsigned)lp * (unsigned)p.page_size));
-    };
-    for (int i = tid; i < (r1 - r0) * GR; i += 256) {
-      const int t = i / GR, g = i % GR;
-      const long long at = token_at(first + t);
-      if (at < 0) continue;
-      const u32x4 codes = *reinterpret_cast<const u32x4*>(c.k_codes + at * (DH / 2) + g * 16);
-      const float sc = q4_key_scale(c.k_scales[at * GR + g]);
-      T* dst = k_out + ((long long)(r0 + t) * p.Hkv + head) * DH + g * 32;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        float x[8];
-        q4_to_f32(codes[j], sc, x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) Elem<T>::store(dst + 8 * j + e, x[e]);
-      }
-    }
-    // eight slots at a time, from a multiple of eight on
-    const long long u0 = first >= 0 ? first / 8 : (first - 7) / 8;
-    const int units = (int)((first + (r1 - r0) + 7 - u0 * 8) / 8);
-    for (int i = tid; i < units * 32; i += 256) {
-      const int j = i & 31;
-      const long long base = (u0 + i / 32) * 8;
-      const long long inside = base < first ? first : base;        // a position of the unit that is asked for
-      const long long at = token_at(inside);
-      if (at < 0) continue;
-      const long long eight = at - (inside - base);
-      const unsigned* src = reinterpret_cast<const unsigned*>(c.v_codes + (eight / 16 * 16) * (DH / 2) + ((eight / 8 & 1) * 32 + j) * GR * 4);
-#pragma unroll
-      for (int cc = 0; cc < GR; ++cc) {
-        float x[8];
-        q4_to_f32(src[cc], 1.f, x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const long long t = base + e - first;
-          if (t < 0 || t >= r1 - r0) continue;
-          Elem<T>::store(v_out + ((long long)(r0 + t) * p.Hkv + head) * DH + 32 * cc + j, x[e] * bf16_to_f32(c.v_scales[eight + e]));
-        }
-      }
-    }
+      if (page >= 0 && page < p.num_pages) at = q4_token(c, page, head, p.page_size, (int)((unsigned)pos - (unsigned)lp * (unsigned)p.page_size));
+      else bad = true;
+    } else bad = true;
+    if (bad && asked) flag_status(p.status, FD_DEV_PAGE_RANGE);
+    where[tid] = at;
+    vscale[tid] = at >= 0 ? bf16_to_f32(c.v_scales[at]) : 0.f;
   }
-  if (bad) flag_status(p.status, FD_DEV_PAGE_RANGE);
+  __syncthreads();
+  {
+    const int u = tid / 32, j = tid % 32;              // (eight tokens that share their words lie in one page)
+    const long long at = where[8 * u];
+    unsigned w[GR] = {};
+    if (at >= 0) {
+      const unsigned char* src = c.v_codes + (at & ~15ll) * (DH / 2) + ((at >> 3 & 1) * 32 + j) * GR * 4;
+      if (GR == 4) { const u32x4 x = *reinterpret_cast<const u32x4*>(src); w[0] = x[0]; w[1] = x[1]; w[GR - 2] = x[2]; w[GR - 1] = x[3]; }
+      else { const u32x2 x = *reinterpret_cast<const u32x2*>(src); w[0] = x[0]; w[1] = x[1]; }
+    }
+#pragma unroll
+    for (int cc = 0; cc < GR; ++cc) vcodes[u][j * GR + cc] = w[cc];
+  }
+  const int g = tid % LPT;
+  constexpr int PASSES = AQ_TOKENS * LPT / 256;
+  unsigned kc[PASSES], ks[PASSES];
+#pragma unroll
+  for (int u = 0; u < PASSES; ++u) {
+    const long long at = where[u * (256 / LPT) + tid / LPT];
+    kc[u] = 0; ks[u] = 127;
+    if (at >= 0) { kc[u] = *reinterpret_cast<const unsigned*>(c.k_codes + at * (DH / 2) + g * 4); ks[u] = c.k_scales[at * GR + g / 4]; }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < PASSES; ++u) {
+    const int t = u * (256 / LPT) + tid / LPT;
+    if (where[t] < 0 || shift + t < 0 || shift + t >= n) continue;
+    const long long row = ((o0 + shift + t) * p.Hkv + head) * (long long)DH + g * 8;
+    float x[8];
+    q4_to_f32(kc[u], q4_key_scale(ks[u]), x);
+    store8(k_out + row, x);
+    // the token's nibble of eight channels' words: channels 8 g .. have c = g / 4, j from 8 (g % 4) on
+    const unsigned* w = &vcodes[t / 8][8 * (g % 4) * GR + g / 4];
+    unsigned v = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v |= ((w[e * GR] >> (4 * (t % 8))) & 15u) << (4 * e);
+    q4_to_f32(v, 1.f, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] *= vscale[t];
+    store8(v_out + row, x);
+  }
 }
 
 template <typename T>
 static void launch_read(const ReadParams& p, const Q4Cache& c, int head_dim, void* k_out, void* v_out, hipStream_t st) {
-  const dim3 grid((p.total_rows + AQ_TOKENS - 1) / AQ_TOKENS, p.Hkv);
+  // 64 tokens each; a sequence begins with up to seven that are not asked for, and ends in part of 64
+  const dim3 grid((unsigned)((long long)p.total_rows / AQ_TOKENS + 2ll * (p.B < p.total_rows ? p.B : p.total_rows)), p.Hkv);
   if (head_dim == 128) hipLaunchKernelGGL((read_kv_q4_kernel<128, T>), grid, dim3(256), 0, st, p, c, reinterpret_cast<T*>(k_out), reinterpret_cast<T*>(v_out));
   else hipLaunchKernelGGL((read_kv_q4_kernel<64, T>), grid, dim3(256), 0, st, p, c, reinterpret_cast<T*>(k_out), reinterpret_cast<T*>(v_out));
 }

@@ -363,33 +363,30 @@ def fd_qk_norm_rope(q, k, q_out, k_out, positions, inv_freq, *, q_weight=None, k
     """q [R, Hq, D], k (and v) [R, Hkv, D]: any strides between rows and heads; outputs dense.  rotary_dim is twice the number of
     inv_freq's entries (None: no rotation)."""
     R, Hq, D = q.shape
-    Hkv = k.shape[1]
-    for name, t, heads in (("q", q, Hq), ("k", k, Hkv), ("v", v, Hkv), ("q_out", q_out, Hq), ("k_out", k_out, Hkv), ("v_out", v_out, Hkv)):
-        if t is None:
-            continue
-        if tuple(t.shape) != (R, heads, D) or t.dtype != q.dtype or (t.numel() and t.stride(2) != 1):
-            raise TypeError(f"{name} must be [{R}, {heads}, {D}] of {q.dtype} with a contiguous last dimension")
-        if name.endswith("_out") and not t.is_contiguous():
-            raise TypeError(f"{name} must be contiguous")
+    Hkv, dt = k.shape[1], q.dtype
+    qs, ks = q.stride(), k.stride()
+    vs = (0, 0, 1) if v is None else v.stride()
+    if not (k.shape == k_out.shape == (R, Hkv, D) and q_out.shape == q.shape and k.dtype == dt and q_out.dtype == dt and k_out.dtype == dt):
+        raise TypeError(f"q, q_out must be [{R}, {Hq}, {D}] and k, k_out [{R}, {Hkv}, {D}], all of {dt}")
+    if (qs[2] != 1 and R * Hq) or (ks[2] != 1 and R * Hkv) or (vs[2] != 1 and R * Hkv):
+        raise TypeError("q, k and v need a contiguous last dimension")
+    if not (q_out.is_contiguous() and k_out.is_contiguous()):
+        raise TypeError("q_out and k_out must be contiguous")
+    if v is not None and not (v_out is not None and v.shape == v_out.shape == k.shape and v.dtype == v_out.dtype == dt and v_out.is_contiguous()):
+        raise TypeError(f"v and v_out must be [{R}, {Hkv}, {D}] of {dt}, v_out contiguous")
     for name, t in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if t is not None and (t.numel() != D or t.dtype != q.dtype or not t.is_contiguous()):
-            raise TypeError(f"{name} must be {D} contiguous elements of {q.dtype}")
-    if inv_freq is not None and (inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous()):
-        raise TypeError("inv_freq must be contiguous float32")
-    if inv_freq is not None and inv_freq.numel() and (positions is None or positions.numel() != R):
-        raise TypeError(f"positions must have {R} entries")
-    a = fd_rope_args()
-    a.total_rows = R; a.num_q_heads = Hq; a.num_kv_heads = Hkv; a.head_dim = D
-    a.rotary_dim = 0 if inv_freq is None else 2 * inv_freq.numel()
-    a.interleaved = 1 if interleaved else 0; a.dtype = _dtype_code(q); a.eps = float(eps)
-    a.q = q.data_ptr(); a.k = k.data_ptr(); a.v = _ptr(v)
-    a.q_stride_row, a.q_stride_head = q.stride(0), q.stride(1)
-    a.k_stride_row, a.k_stride_head = k.stride(0), k.stride(1)
-    if v is not None:
-        a.v_stride_row, a.v_stride_head = v.stride(0), v.stride(1)
-    a.q_out = q_out.data_ptr(); a.k_out = k_out.data_ptr(); a.v_out = _ptr(v_out)
-    a.q_weight = _ptr(q_weight); a.k_weight = _ptr(k_weight); a.inv_freq = _ptr(inv_freq)
-    a.positions = _opt_i32(positions, "positions")
+        if t is not None and (t.numel() != D or t.dtype != dt or not t.is_contiguous()):
+            raise TypeError(f"{name} must be {D} contiguous elements of {dt}")
+    half = 0
+    if inv_freq is not None:
+        half = inv_freq.numel()
+        if inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous():
+            raise TypeError("inv_freq must be contiguous float32")
+        if half and (positions is None or positions.numel() != R):
+            raise TypeError(f"positions must have {R} entries")
+    a = fd_rope_args(R, Hq, Hkv, D, 2 * half, 1 if interleaved else 0, _dtype_code(q), eps, q.data_ptr(), k.data_ptr(), _ptr(v), qs[0], qs[1], ks[0], ks[1],
+                     vs[0], vs[1], q_out.data_ptr(), k_out.data_ptr(), _ptr(v_out), _ptr(q_weight), _ptr(k_weight), _ptr(inv_freq),
+                     _opt_i32(positions, "positions"))
     _check(load().fd_qk_norm_rope(C.byref(a), _stream(stream)))
 
 
@@ -457,14 +454,14 @@ def fd_append_kv_q4(args: fd_attn_args, cache: Q4Cache, accept_len, kv_len_out, 
 
 def fd_read_kv_q4(cache: Q4Cache, page_indptr, page_indices, start, out_indptr, k_out, v_out, *, status=None, stream=None) -> None:
     """Tokens start[i] .. of every sequence as rows out_indptr[i] .. of k_out / v_out [R, Hkv, D], float32 or bfloat16."""
-    shape = (k_out.shape[0], cache.num_kv_heads, cache.head_dim)
-    for name, t in (("k_out", k_out), ("v_out", v_out)):
-        if tuple(t.shape) != shape or not t.is_contiguous() or t.dtype != k_out.dtype:
-            raise TypeError(f"{name} must be contiguous, of shape {shape}, both of one dtype")
+    R = k_out.shape[0]
+    if not (k_out.shape == v_out.shape == (R, cache.num_kv_heads, cache.head_dim) and k_out.dtype == v_out.dtype and k_out.is_contiguous() and
+            v_out.is_contiguous()):
+        raise TypeError(f"k_out and v_out must be contiguous, [rows, {cache.num_kv_heads}, {cache.head_dim}], both of one dtype")
     _check(load().fd_read_kv_q4(
         C.byref(cache.c), out_indptr.shape[0] - 1, cache.num_kv_heads, cache.head_dim, cache.page_size, cache.num_pages,
         _ptr(_i32(page_indptr, "page_indptr")), _ptr(_i32(page_indices, "page_indices")), page_indices.numel(), _opt_i32(start, "start"),
-        _ptr(_i32(out_indptr, "out_indptr")), k_out.shape[0], _ptr(k_out), _ptr(v_out), _dtype_code(k_out), _ptr(status), _stream(stream)))
+        _ptr(_i32(out_indptr, "out_indptr")), R, _ptr(k_out), _ptr(v_out), _dtype_code(k_out), _ptr(status), _stream(stream)))
 
 
 def fd_version() -> str:
