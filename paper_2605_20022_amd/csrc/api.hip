@@ -524,15 +524,16 @@ fd_status fd_qk_norm_rope(const fd_rope_args* a, void* hip_stream) {
   return FD_OK;
 }
 
-static fd_status check_q4_cache(const fd_q4_cache* c, int head_dim, int page_size, int num_kv_heads) {
+static fd_status check_q4_cache(const fd_q4_cache* c, int head_dim, int page_size, int num_kv_heads, int num_pages) {
   if (!c) return fail(FD_ERR_INVALID_ARG, "cache is NULL");
   if (head_dim != 128 && head_dim != 64) return fail(FD_ERR_UNSUPPORTED, "a cache in 4 bits has head_dim 128 or 64, not %d", head_dim);
   if (page_size <= 0 || page_size % 16) return fail(page_size <= 0 ? FD_ERR_INVALID_ARG : FD_ERR_UNSUPPORTED, "page_size %d of a cache in 4 bits must be a positive multiple of 16", page_size);
   if (num_kv_heads <= 0 || num_kv_heads > 65535) return fail(FD_ERR_INVALID_ARG, "num_kv_heads %d", num_kv_heads);
   if (c->stride_page < 0 || c->stride_head < 0 || c->stride_page >= (1ll << 31) || c->stride_head >= (1ll << 31))
     return fail(FD_ERR_INVALID_ARG, "cache strides must be in [0, 2^31) blocks");
-  if (c->stride_page * page_size >= (1ll << 31) || c->stride_head * page_size >= (1ll << 31))
-    return fail(FD_ERR_UNSUPPORTED, "cache strides of 2^31 tokens or more");
+  // tokens are numbered in 32 bits (an array of 2^32 of them takes more memory than there is)
+  if ((double)page_size * ((double)(num_pages > 0 ? num_pages - 1 : 0) * c->stride_page + (double)(num_kv_heads - 1) * c->stride_head + 1.0) > 4294967296.0)
+    return fail(FD_ERR_UNSUPPORTED, "a cache of more than 2^32 tokens and heads");
   if (!aligned16(c->k_codes) || !aligned16(c->v_codes) || !aligned16(c->v_scales) || (reinterpret_cast<uintptr_t>(c->k_scales) & 3))
     return fail(FD_ERR_INVALID_ARG, "k_codes, v_codes and v_scales must be 16-byte aligned, k_scales 4-byte aligned");
   return FD_OK;
@@ -599,7 +600,7 @@ fd_status fd_verify_draft_attn_q4(const fd_attn_args* a, const fd_q4_cache* cach
   size_t need = 0;
   fd_status st = plan_attn_q4(a, &need);
   if (st != FD_OK) return st;
-  st = check_q4_cache(cache, a->head_dim, a->page_size, a->num_kv_heads);
+  st = check_q4_cache(cache, a->head_dim, a->page_size, a->num_kv_heads, a->num_pages);
   if (st != FD_OK) return st;
   g_err[0] = 0;
   if (a->batch == 0 || a->total_rows == 0) return FD_OK;          // nothing to compute
@@ -621,7 +622,7 @@ fd_status fd_verify_draft_attn_q4(const fd_attn_args* a, const fd_q4_cache* cach
 fd_status fd_append_kv_q4(const fd_attn_args* a, const fd_q4_cache* cache, const int32_t* accept_len, int32_t* kv_len_out, void* hip_stream) {
   fd_status st = check_q4_args(a);
   if (st != FD_OK) return st;
-  st = check_q4_cache(cache, a->head_dim, a->page_size, a->num_kv_heads);
+  st = check_q4_cache(cache, a->head_dim, a->page_size, a->num_kv_heads, a->num_pages);
   if (st != FD_OK) return st;
   if (a->max_new_rows > 65535) return fail(FD_ERR_UNSUPPORTED, "max_new_rows %d > 65535", a->max_new_rows);
   g_err[0] = 0;
@@ -645,7 +646,7 @@ fd_status fd_read_kv_q4(const fd_q4_cache* cache, int32_t batch, int32_t num_kv_
   if (batch < 0 || num_pages < 0 || page_indices_len < 0 || total_rows < 0) return fail(FD_ERR_INVALID_ARG, "negative size");
   if (batch > 65535) return fail(FD_ERR_UNSUPPORTED, "batch %d > 65535", batch);
   if (out_dtype != FD_F32 && out_dtype != FD_BF16) return fail(FD_ERR_INVALID_ARG, "unknown dtype %d", (int)out_dtype);
-  fd_status st = check_q4_cache(cache, head_dim, page_size, num_kv_heads);
+  fd_status st = check_q4_cache(cache, head_dim, page_size, num_kv_heads, num_pages);
   if (st != FD_OK) return st;
   g_err[0] = 0;
   if (batch == 0 || total_rows == 0) return FD_OK;

@@ -18,6 +18,8 @@
 
 namespace fd {
 
+#define FD_INLINE __attribute__((always_inline))      // on a lambda: what it captures stays in registers
+
 constexpr int Q4_BLOCK = 256;
 constexpr int Q4_TK = 32;                 // keys of a block
 constexpr int Q4_ROWS = 128;              // tile rows of an item
@@ -169,51 +171,47 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
   // ---- cached keys: which blocks, where they lie ----
   const int lo = first + slot, hi = min(last, cached);
   const int count = lo < hi ? (hi - lo + KS - 1) >> ks_shift : 0;        // blocks of this wave: lo, lo + KS, ...
-  // The pages of the wave's block t, sixteen keys each; for what lies past the last block or the prefix, those of keys that are there.
-  struct Pages { int page[2], slot[2]; };
-  auto find_pages = [&](int t) {
-    Pages r;
-    const int pos = 32 * (lo + (min(t, count - 1) << ks_shift));
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const int x = q ? min(pos + 16, (s.L - 1) & ~15) : pos;
-      const int lp = (int)(__umulhi((unsigned)x, p.page_magic) >> p.page_magic_shift);
-      r.slot[q] = x - lp * p.page_size;
-      r.page[q] = sload(p.page_indices, s.page0 + lp);
-    }
-    return r;
+  // Where the two sixteens of the wave's block t lie, as token numbers (q4_token; the host has seen to it that they fit 32 bits): lane t % 64 knows
+  // it.  For what lies past the last block or the prefix: keys that are there.
+  const unsigned page_tokens = (unsigned)c.sp * (unsigned)p.page_size, head_tokens = (unsigned)c.sh * (unsigned)p.page_size * (unsigned)pc.head;
+  auto page_of = [&](int pos, unsigned& slot) FD_INLINE -> int {
+    const int lp = (int)(__umulhi((unsigned)pos, p.page_magic) >> p.page_magic_shift);
+    slot = (unsigned)(pos - lp * p.page_size);
+    return p.page_indices[s.page0 + lp];
   };
-  // Where sixteen keys lie.  The host has seen to it that a page's and a head's tokens fit 31 bits, so a product of 32 bits by 32 is all it takes.
-  struct Tokens { unsigned long long at[2]; };
-  const unsigned page_tokens = (unsigned)c.sp * (unsigned)p.page_size;
-  const unsigned long long head_tokens = (unsigned long long)((unsigned)c.sh * (unsigned)p.page_size) * (unsigned)pc.head;
-  unsigned bad_page = 0;
-  auto tokens = [&](const Pages& r) {
-    Tokens t;
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const bool bad = (unsigned)r.page[q] >= (unsigned)p.num_pages;
-      bad_page |= bad;
-      t.at[q] = (unsigned long long)(bad ? 0u : (unsigned)r.page[q]) * page_tokens + (head_tokens + (unsigned)r.slot[q]);
-    }
-    return t;
+  auto token_of = [&](int page, unsigned slot) FD_INLINE -> unsigned {
+    const bool bad = (unsigned)page >= (unsigned)p.num_pages;
+    if (bad) flag_status(p.status, FD_DEV_PAGE_RANGE);
+    return (bad ? 0u : (unsigned)page) * page_tokens + head_tokens + slot;
+  };
+  unsigned where0 = 0, where1 = 0;
+  auto find_pages = [&](int t) FD_INLINE {                         // t: a multiple of 64
+    const int pos = 32 * (lo + (min(t + lane, count - 1) << ks_shift));
+    unsigned slot0, slot1;
+    const int page0 = page_of(pos, slot0), page1 = page_of(min(pos + 16, (s.L - 1) & ~15), slot1);
+    where0 = token_of(page0, slot0);
+    where1 = token_of(page1, slot1);
+  };
+  auto look_up = [&](int t, unsigned& at0, unsigned& at1) FD_INLINE {
+    if ((t & 63) == 0 && t > 0) find_pages(t);
+    at0 = __builtin_amdgcn_readlane(where0, t & 63);
+    at1 = __builtin_amdgcn_readlane(where1, t & 63);
   };
   const int key_of_row = (l31 & 16) | ((l31 & 4) << 1) | ((l31 & 8) >> 1) | (l31 & 3);
-  const unsigned k_off = (key_of_row & 15) * (DH / 2) + h * 16, ks_off = (key_of_row & 15) * (DH / 32);
-  auto request_keys = [&](Q4Keys<DH>& r, const Tokens& at) {
-    const unsigned char* k0 = c.k_codes + at.at[0] * (DH / 2); const unsigned char* k1 = c.k_codes + at.at[1] * (DH / 2);
-    const unsigned char* k = (key_of_row & 16 ? k1 : k0) + k_off;
-    const unsigned char* s0 = c.k_scales + at.at[0] * (DH / 32); const unsigned char* s1 = c.k_scales + at.at[1] * (DH / 32);
-    const unsigned char* ks = (key_of_row & 16 ? s1 : s0) + ks_off;
+  auto request_keys = [&](Q4Keys<DH>& r, unsigned at0, unsigned at1) FD_INLINE {
+    const unsigned mine = (key_of_row & 16 ? at1 : at0) + (unsigned)(key_of_row & 15);
+    const unsigned char* k = c.k_codes + (unsigned long long)mine * (DH / 2) + h * 16;
 #pragma unroll
     for (int a = 0; a < NA; ++a) r.code[a] = *reinterpret_cast<const u32x4*>(k + 32 * a);
+    const unsigned char* ks = c.k_scales + (unsigned long long)mine * (DH / 32);
     if (DH == 128) r.scale = *reinterpret_cast<const unsigned*>(ks);
     else r.scale = *reinterpret_cast<const unsigned short*>(ks);
   };
-  auto request_values = [&](Q4Values<DH>& r, const Tokens& at) {
+  auto request_values = [&](Q4Values<DH>& r, unsigned at0, unsigned at1) FD_INLINE {
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      const unsigned char* v = c.v_codes + at.at[q] * (DH / 2);
+      const unsigned tok = q ? at1 : at0;
+      const unsigned char* v = c.v_codes + (unsigned long long)tok * (DH / 2);
       if (DH == 128) {
         const u32x4 x = *reinterpret_cast<const u32x4*>(v + (unsigned)lane * 16u);
 #pragma unroll
@@ -222,14 +220,12 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
         const u32x2 x = *reinterpret_cast<const u32x2*>(v + (unsigned)lane * 8u);
         r.code[q][0] = x[0]; r.code[q][1] = x[1];
       }
-      r.scale[q] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const unsigned char*>(c.v_scales) + at.at[q] * 2 + (unsigned)h * 16u);
+      r.scale[q] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const unsigned char*>(c.v_scales) + (unsigned long long)tok * 2 + (unsigned)h * 16u);
     }
   };
   Q4Keys<DH> ka, kb;
   Q4Values<DH> va, vb;
-  Pages pg = {};
-  Tokens tok = {};
-  if (count > 0) pg = find_pages(0);
+  if (count > 0) find_pages(0);
 
   // ---- this lane's row and its query, as the second operand of S^T = K Q^T ----
   const int tr = rb * 32 + l31;
@@ -241,14 +237,13 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
 #pragma unroll
   for (int t = 0; t < 4 * NA; ++t) qw[t] = *reinterpret_cast<const u32x4*>(qrow + 64 * (t / 4) + 32 * (t / 2 % 2) + 16 * h + 8 * (t % 2));
   if (count > 0) {
-    const Pages p1 = find_pages(1), p2 = find_pages(2);
-    tok = tokens(pg);
-    request_keys(ka, tok);
-    request_values(va, tok);
-    pg = p2;
-    tok = tokens(p1);
-    request_keys(kb, tok);
-    request_values(vb, tok);
+    unsigned at0, at1;
+    look_up(0, at0, at1);
+    request_keys(ka, at0, at1);
+    request_values(va, at0, at1);
+    look_up(1, at0, at1);
+    request_keys(kb, at0, at1);
+    request_values(vb, at0, at1);
   }
   // The query as the sum of two e4m3 numbers: q = 2^u hi + 2^(u-5) lo with 2^u hi up to 2^(u+8) the row's largest magnitude.  hi keeps four significant
   // bits, what is left of a bf16's eight fits four more: exact for all but elements 2^-14 of the largest, and those to 2^-22 of it.
@@ -295,9 +290,9 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
   // Scores -> probabilities.  They are taken against the running maximum as it stands; only where a row's sixteen sum to more than
   // Q4_LAZY (the first block does) is the maximum found, and what was summed so far shrunk to it.  Sums and bf16 probabilities have the same
   // relative precision whatever the reference, and a maximum costs as much as half the exponentials.
-  auto softmax = [&](f32x16& x) {
+  auto softmax = [&](f32x16& x) FD_INLINE {
     f32x16 y;
-    auto exponentials = [&]() {
+    auto exponentials = [&]() FD_INLINE {
       float t[4];
 #pragma unroll
       for (int e = 0; e < 16; ++e) y[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], scale2, -m));
@@ -322,7 +317,7 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
     l += sum;
     x = y;
   };
-  auto key_scores = [&](const Q4Keys<DH>& r) {
+  auto key_scores = [&](const Q4Keys<DH>& r) FD_INLINE {
     f32x16 x;
 #pragma unroll
     for (int e = 0; e < 16; ++e) x[e] = 0.f;
@@ -331,7 +326,7 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
     if (NA == 2) x = scores<2>(r.code[NA - 1], ks, qh[NA - 1], ql[NA - 1], uh, ul, x);
     return x;
   };
-  auto weigh_values = [&](f32x16 x, Q4Values<DH>& r, int left) {        // left: keys of the block, if below 32
+  auto weigh_values = [&](f32x16 x, Q4Values<DH>& r, int left) FD_INLINE {        // left: keys of the block, if below 32
     if (left < 32) {                                     // a slot behind the prefix holds anything, a NaN as its scale too
       asm volatile("");                                  // (a branch: as selects this would run for every block)
 #pragma unroll
@@ -362,25 +357,23 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  // Keys and values of two blocks are held or on their way, the pages of a third are looked up.  Past the end the last block is requested again (its
-  // lines are at hand), so that nothing in the loop depends on the count; with an odd count the last step's second half weighs nothing.
+  // Keys and values of two blocks are held or on their way.  Past the end the last block is requested again (its lines are at hand), so that
+  // nothing in the loop depends on the count; with an odd count the last step's second half weighs nothing.
   if (count > 0) {
     const int left0 = s.L - 32 * lo, step = 32 << ks_shift;
     for (int t = 0; t < count; t += 2) {
       f32x16 x = key_scores(ka);
-      tok = tokens(pg);
-      pg = find_pages(t + 3);
-      request_keys(ka, tok);
+      unsigned at0, at1;
+      look_up(t + 2, at0, at1);
+      request_keys(ka, at0, at1);
       weigh_values(x, va, left0 - t * step);
-      request_values(va, tok);
+      request_values(va, at0, at1);
       x = key_scores(kb);
-      tok = tokens(pg);
-      pg = find_pages(t + 4);
-      request_keys(kb, tok);
+      look_up(t + 3, at0, at1);
+      request_keys(kb, at0, at1);
       weigh_values(x, vb, t + 1 < count ? left0 - (t + 1) * step : 0);
-      request_values(vb, tok);
+      request_values(vb, at0, at1);
     }
-    if (bad_page && lane == 0) flag_status(p.status, FD_DEV_PAGE_RANGE);
   }
 
   // ---- the sequence's own rows, in bf16: keys as the first operand straight from memory, values through this wave's part of LDS and its transposing read ----
@@ -399,12 +392,12 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
 #pragma unroll
     for (int t = 0; t < STEPS; ++t) qf[t] = *reinterpret_cast<const u32x4*>(qrow + 64 * (t / 4) + 32 * h + 8 * (t % 4));
     // (behind the last row: that row, which the mask leaves out)
-    auto load_k = [&](int t0) {
+    auto load_k = [&](int t0) FD_INLINE {
       const bf16_t* krow = k0 + min(t0 + key_of_row, s.n - 1) * stride;
 #pragma unroll
       for (int t = 0; t < STEPS; ++t) kf[t] = *reinterpret_cast<const u32x4*>(krow + 64 * (t / 4) + 32 * h + 8 * (t % 4));
     };
-    auto load_v = [&](int t0) {
+    auto load_v = [&](int t0) FD_INLINE {
 #pragma unroll
       for (int t = 0; t < STEPS; ++t) vr[t] = *reinterpret_cast<const u32x4*>(v0 + min(t0 + RPL * t + lane / LPR, s.n - 1) * stride + lane % LPR * 8);
     };
