@@ -131,14 +131,13 @@ __device__ __forceinline__ float add_halves(float x) {
 }
 
 typedef __attribute__((ext_vector_type(8))) int i32x8;
-// x += K Q^T over 64 channels: 32 codes of a key with their scale (byte BYTE of ks) and the two parts of the query.
+// x += K q^T over 64 channels: 32 codes of a key with their scale (byte BYTE of ks) and one part of the query with its exponent.
 template <int BYTE>
-__device__ __forceinline__ f32x16 scores(u32x4 k, unsigned ks, i32x8 qh, i32x8 ql, int uh, int ul, f32x16 x) {
+__device__ __forceinline__ f32x16 scores(u32x4 k, unsigned ks, i32x8 q, int u, f32x16 x) {
   typedef __attribute__((ext_vector_type(4))) int i32x4;
   const i32x4 k4 = __builtin_bit_cast(i32x4, k);
   const i32x8 a = __builtin_shufflevector(k4, k4, 0, 1, 2, 3, -1, -1, -1, -1);
-  x = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, ql, x, 4, 0, BYTE, (int)ks, 0, ul);       // formats: 4 = e2m1, 0 = e4m3
-  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, qh, x, 4, 0, BYTE, (int)ks, 0, uh);
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, q, x, 4, 0, BYTE, (int)ks, 0, u);       // formats: 4 = e2m1, 0 = e4m3
 }
 
 // Codes and scales of a block as a lane holds them.
@@ -290,17 +289,15 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
   // Scores -> probabilities.  They are taken against the running maximum as it stands; only where a row's sixteen sum to more than
   // Q4_LAZY (the first block does) is the maximum found, and what was summed so far shrunk to it.  Sums and bf16 probabilities have the same
   // relative precision whatever the reference, and a maximum costs as much as half the exponentials.
-  auto softmax = [&](f32x16& x) FD_INLINE {
-    f32x16 y;
-    auto exponentials = [&]() FD_INLINE {
-      float t[4];
+  auto exponentials = [&](const f32x16& x, f32x16& y) FD_INLINE {
+    float t[4];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) y[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], scale2, -m));
+    for (int e = 0; e < 16; ++e) y[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], scale2, -m));
 #pragma unroll
-      for (int e = 0; e < 4; ++e) t[e] = (y[4 * e] + y[4 * e + 1]) + (y[4 * e + 2] + y[4 * e + 3]);
-      return (t[0] + t[1]) + (t[2] + t[3]);
-    };
-    float sum = exponentials();
+    for (int e = 0; e < 4; ++e) t[e] = (y[4 * e] + y[4 * e + 1]) + (y[4 * e + 2] + y[4 * e + 3]);
+    return (t[0] + t[1]) + (t[2] + t[3]);
+  };
+  auto settle = [&](const f32x16& x, f32x16& y, float sum) FD_INLINE {
     if (__any(sum > Q4_LAZY)) {
       float top = x[0];
 #pragma unroll
@@ -312,21 +309,26 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
       for (int cc = 0; cc < NC; ++cc)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[cc][e] *= f;
-      sum = exponentials();
+      sum = exponentials(x, y);
     }
     l += sum;
-    x = y;
   };
   auto key_scores = [&](const Q4Keys<DH>& r) FD_INLINE {
     f32x16 x;
 #pragma unroll
     for (int e = 0; e < 16; ++e) x[e] = 0.f;
     const unsigned ks = r.scale >> (8 * h);
-    x = scores<0>(r.code[0], ks, qh[0], ql[0], uh, ul, x);
-    if (NA == 2) x = scores<2>(r.code[NA - 1], ks, qh[NA - 1], ql[NA - 1], uh, ul, x);
+    x = scores<0>(r.code[0], ks, ql[0], ul, x);
+    x = scores<0>(r.code[0], ks, qh[0], uh, x);
+    if (NA == 2) {
+      x = scores<2>(r.code[NA - 1], ks, ql[NA - 1], ul, x);
+      x = scores<2>(r.code[NA - 1], ks, qh[NA - 1], uh, x);
+    }
     return x;
   };
-  auto weigh_values = [&](f32x16 x, Q4Values<DH>& r, int left) FD_INLINE {        // left: keys of the block, if below 32
+  // One block: its scores x become probabilities and weigh its values, while the matrix pipe works on the scores of the next.  left: keys of the
+  // block, if below 32.
+  auto block = [&](f32x16 x, Q4Values<DH>& r, const Q4Keys<DH>& next, int left) FD_INLINE {
     if (left < 32) {                                     // a slot behind the prefix holds anything, a NaN as its scale too
       asm volatile("");                                  // (a branch: as selects this would run for every block)
 #pragma unroll
@@ -339,13 +341,34 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
         r.scale[e / 4][e % 4] = key >= left ? 0u : key + 1 >= left ? w & 0xffffu : w;
       }
     }
-    softmax(x);
+    // a product for the next scores, then a share of the exponentials, in this order
+    f32x16 y, xn;
+    float part[2 * NA];
+    const unsigned ks = next.scale >> (8 * h);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) xn[e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < 2 * NA; ++i) {
+      constexpr int SHARE = 16 / (2 * NA);
+      __builtin_amdgcn_sched_barrier(0);
+      xn = i % 2 == 0 ? (i < 2 ? scores<0>(next.code[0], ks, ql[0], ul, xn) : scores<2>(next.code[NA - 1], ks, ql[NA - 1], ul, xn))
+                      : (i < 2 ? scores<0>(next.code[0], ks, qh[0], uh, xn) : scores<2>(next.code[NA - 1], ks, qh[NA - 1], uh, xn));
+      __builtin_amdgcn_sched_barrier(0);
+      part[i] = 0.f;
+#pragma unroll
+      for (int e = i * SHARE; e < (i + 1) * SHARE; ++e) y[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], scale2, -m));
+#pragma unroll
+      for (int e = i * SHARE; e < (i + 1) * SHARE; e += 2) part[i] = e == i * SHARE ? y[e] + y[e + 1] : part[i] + (y[e] + y[e + 1]);
+    }
+    const float sum = NA == 2 ? (part[0] + part[1]) + (part[2 * NA - 2] + part[2 * NA - 1]) : part[0] + part[1];
+    asm volatile("" : "+v"(xn));                         // (not to be moved past the branch)
+    settle(x, y, sum);
     u32x4 pf[2];                                         // P times the values' scales
 #pragma unroll
     for (int q = 0; q < 2; ++q)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        pf[q][e] = pack_bf16x2(x[8 * q + 2 * e] * __uint_as_float(r.scale[q][e] << 16), x[8 * q + 2 * e + 1] * __uint_as_float(r.scale[q][e] & 0xffff0000u));
+        pf[q][e] = pack_bf16x2(y[8 * q + 2 * e] * __uint_as_float(r.scale[q][e] << 16), y[8 * q + 2 * e + 1] * __uint_as_float(r.scale[q][e] & 0xffff0000u));
     // codes are converted one product ahead, so that the matrix pipe does not wait for them
     u32x4 vf[2];
     vf[0] = q4_to_bf16(r.code[0][0], 1.f);
@@ -356,23 +379,25 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
       o[i % NC] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vf[i & 1]), as_bf16x8(pf[i / NC]), o[i % NC], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
     }
+    return xn;
   };
   // Keys and values of two blocks are held or on their way.  Past the end the last block is requested again (its lines are at hand), so that
   // nothing in the loop depends on the count; with an odd count the last step's second half weighs nothing.
   if (count > 0) {
     const int left0 = s.L - 32 * lo, step = 32 << ks_shift;
+    f32x16 x = key_scores(ka);
+    unsigned at0, at1, bt0, bt1;
+    look_up(2, at0, at1);
+    request_keys(ka, at0, at1);
     for (int t = 0; t < count; t += 2) {
-      f32x16 x = key_scores(ka);
-      unsigned at0, at1;
-      look_up(t + 2, at0, at1);
-      request_keys(ka, at0, at1);
-      weigh_values(x, va, left0 - t * step);
+      x = block(x, va, kb, left0 - t * step);
       request_values(va, at0, at1);
-      x = key_scores(kb);
-      look_up(t + 3, at0, at1);
-      request_keys(kb, at0, at1);
-      weigh_values(x, vb, t + 1 < count ? left0 - (t + 1) * step : 0);
-      request_values(vb, at0, at1);
+      look_up(t + 3, bt0, bt1);
+      request_keys(kb, bt0, bt1);
+      x = block(x, vb, ka, t + 1 < count ? left0 - (t + 1) * step : 0);
+      request_values(vb, bt0, bt1);
+      look_up(t + 4, at0, at1);
+      request_keys(ka, at0, at1);
     }
   }
 
@@ -438,7 +463,10 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
         const int t = t0 + 16 * (e / 8) + 8 * h + e % 8;
         x[e] = ((t < s.n) & new_key_visible(win, t)) ? x[e] : -INFINITY;
       }
-      softmax(x);
+      f32x16 y;
+      const float sum = exponentials(x, y);
+      settle(x, y, sum);
+      x = y;
       __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
       // (sixteen lanes read four keys of sixteen channels, and each gets its channel's four)
       const bf16_t* vt = lv + (8 * h + ((lane & 15) >> 2)) * VP + (l31 & 16) + 4 * (lane & 3);
