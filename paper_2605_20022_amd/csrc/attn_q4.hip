@@ -24,16 +24,19 @@ constexpr int Q4_BLOCK = 256;
 constexpr int Q4_TK = 32;                 // keys of a block
 constexpr int Q4_ROWS = 128;              // tile rows of an item
 constexpr float Q4_LAZY = 256.f;          // sum of a row's sixteen probabilities from which on the softmax reference follows the row maximum
-constexpr int Q4_PIECES = 1024;           // pieces aimed at
+constexpr int Q4_SLOTS = 512;             // work-groups that run at once: two a compute unit
+constexpr int Q4_PIECES = 1024;           // pieces aimed at where there are more than Q4_SLOTS / 2 items
 constexpr int Q4_MIN_PIECE = 8;           // blocks of a piece, at least (but for the last of a short item)
+constexpr int Q4_KEPT = 4;                // rounds of 64 sequences whose lengths a wave keeps in registers
 
 struct Q4Sched {
   int fixed;                // > 0: blocks of a piece, asked for by the caller
+  float a_fixed;            // pieces a block, then
   int unit_shift;           // work is counted in 2^unit_shift units
   int rt_max;               // items of a (sequence, head), at most
   int max_partials;         // partial slots in the workspace
-  float* part_acc;          // [max_partials][128][D] un-normalised O
-  float* part_ml;           // [max_partials][128][2] maximum (base 2), sum
+  unsigned short* part_acc; // [max_partials][128][D] fp16: the un-normalised O row divided by its largest magnitude
+  float* part_ml;           // [max_partials][128][4] maximum (base 2), sum, that largest magnitude, unused
   int2* entries;            // [B * Hkv * rt_max]: pieces, first partial slot
 };
 
@@ -42,74 +45,118 @@ __device__ __forceinline__ int q4_row_blocks(int rows) { return rows <= 32 ? 1 :
 // How long a block takes a work-group, in halves: four waves take four blocks of one row block side by side, or one block of four.
 __device__ __forceinline__ int q4_weight(int rows) { return rows <= 32 ? 2 : rows <= 64 ? 3 : 6; }
 
-struct Q4Cut { int blocks, full, tail_rows; };          // of one sequence: blocks of its keys, items of 128 tile rows, rows of the last item
-__device__ __forceinline__ Q4Cut q4_cut(const AttnParams& p, const SeqInfo& s) {
-  Q4Cut c;
-  c.blocks = s.n > 0 ? (s.L + Q4_TK - 1) / Q4_TK + (s.n + Q4_TK - 1) / Q4_TK : 0;
-  const int rows = s.n * p.G;
-  c.full = rows / Q4_ROWS;
-  c.tail_rows = rows - c.full * Q4_ROWS;
-  return c;
+// Blocks of a sequence's keys, and its tile rows: rows / 128 whole items and one of what is left.
+__device__ __forceinline__ int q4_blocks(const SeqInfo& s) { return s.n > 0 ? (s.L + Q4_TK - 1) / Q4_TK + (s.n + Q4_TK - 1) / Q4_TK : 0; }
+__device__ __forceinline__ long long q4_units(int blocks, int rows) {           // of one head: weight x blocks
+  const int tail = rows % Q4_ROWS;
+  return (long long)blocks * (rows / Q4_ROWS * q4_weight(Q4_ROWS) + (tail ? q4_weight(tail) : 0));
 }
-// Pieces of an item of so many rows.  target: units of weight x blocks a piece should have.
-__device__ __forceinline__ int q4_pieces(const Q4Sched& sc, int blocks, int rows, int target) {
+// Pieces of an item: density (pieces a unit) x its units, rounded up, and no piece below Q4_MIN_PIECE blocks.  The products stay a little below the
+// exact ones, so that pieces - 1 never exceeds density x units, which the host counts on.
+__device__ __forceinline__ int q4_pieces(const Q4Sched& sc, int blocks, int rows, float density) {
   if (blocks <= 0 || rows <= 0) return 0;
-  const unsigned w = q4_weight(rows);
-  unsigned per = sc.fixed > 0 ? (unsigned)sc.fixed : ((unsigned)target + w - 1) / w;
-  if (sc.fixed <= 0 && per < Q4_MIN_PIECE) per = Q4_MIN_PIECE;
-  return (int)(((unsigned)blocks + per - 1) / per);
+  const float a_block = sc.fixed > 0 ? sc.a_fixed : fminf(density * (float)q4_weight(rows), 1.f / Q4_MIN_PIECE);
+  return (int)((float)blocks * (a_block * 0.999999f)) + 1;
+}
+struct Q4Count { int full, tail; };       // pieces of a whole item and of the last
+__device__ __forceinline__ Q4Count q4_count(const Q4Sched& sc, int blocks, int rows, float density) {
+  return Q4Count{rows >= Q4_ROWS ? q4_pieces(sc, blocks, Q4_ROWS, density) : 0, q4_pieces(sc, blocks, rows % Q4_ROWS, density)};
 }
 
 struct Q4Piece { int head, rt, piece, pieces, slot, item; SeqInfo s; };
 
 // Which piece work-group w takes: pieces are numbered by (sequence, head, item, piece).  Every wave finds it by itself, a sequence a lane, 64 at a
 // time: the lengths are one latency of memory, the rest lane shifts, and no wave waits for another.  false: none.
+//
+// How many pieces: with at most Q4_SLOTS / 2 items as many as run at once, found by bisection, so that one round does it: a piece's start and
+// end cost about as much as twelve blocks (find, pages, first codes, merge), and a second round would wait for the first.  Else Q4_PIECES and
+// the items themselves, dealt out as work-groups become free.
 __device__ __forceinline__ bool q4_find(const AttnParams& p, const Q4Sched& sc, int w, Q4Piece& out) {
   const int lane = threadIdx.x & 63;
   const int rounds = (p.B + 63) / 64;
-  Q4Cut cut = {};
-  SeqInfo mine = {};
-  auto load = [&](int c) {
-    cut = Q4Cut{};
+  int kept_blocks[Q4_KEPT], kept_rows[Q4_KEPT];
+  auto load = [&](int c, int& blocks, int& rows) FD_INLINE {
     uint32_t bad = 0;
     const int i = c * 64 + lane;
-    if (i < p.B) { mine = load_seq_t<false>(p, i, &bad); cut = q4_cut(p, mine); }
+    blocks = rows = 0;
+    if (i < p.B) {
+      const SeqInfo s = load_seq_t<false>(p, i, &bad);
+      blocks = q4_blocks(s);
+      rows = s.n * p.G;
+    }
     if (bad && w == 0 && threadIdx.x < 64) flag_status(p.status, bad);        // (work-group 0 comes by every sequence)
   };
-  int total = 0;                                         // units of weight x blocks of one head, in 2^unit_shift (the host's bounds say that they fit)
-  for (int c = 0; c < rounds; ++c) {
-    load(c);
-    const long long units = (long long)cut.blocks * (cut.full * q4_weight(Q4_ROWS) + (cut.tail_rows ? q4_weight(cut.tail_rows) : 0));
-    total += wave_total((int)((units + (1ll << sc.unit_shift) - 1) >> sc.unit_shift));      // (up, so that there are never more pieces than the host counts on)
+  int total = 0, items = 0;                              // units of one head, in 2^unit_shift (the host's bounds say that they fit), and items
+  auto add = [&](int blocks, int rows) FD_INLINE {
+    // (rounded up, so that there are never more pieces than the host counts on)
+    total += wave_total((int)((q4_units(blocks, rows) + (1ll << sc.unit_shift) - 1) >> sc.unit_shift));
+    items += wave_total((rows + Q4_ROWS - 1) / Q4_ROWS);
+  };
+#pragma unroll
+  for (int c = 0; c < Q4_KEPT; ++c) {
+    kept_blocks[c] = kept_rows[c] = 0;
+    if (c < rounds) load(c, kept_blocks[c], kept_rows[c]);
   }
-  const long long share = (((long long)total << sc.unit_shift) * p.Hkv + Q4_PIECES - 1) / Q4_PIECES;
-  const int per_piece = share < 1 ? 1 : share < (1 << 30) ? (int)share : 1 << 30;
+#pragma unroll
+  for (int c = 0; c < Q4_KEPT; ++c)
+    if (c < rounds) add(kept_blocks[c], kept_rows[c]);
+  for (int c = Q4_KEPT; c < rounds; ++c) {
+    int blocks, rows;
+    load(c, blocks, rows);
+    add(blocks, rows);
+  }
+  const float all = ldexpf((float)total, sc.unit_shift) * (float)p.Hkv * 1.000001f;
+  float density = (float)Q4_PIECES / fmaxf(all, 1.f);
+  if (sc.fixed <= 0 && items * (long long)p.Hkv <= Q4_SLOTS / 2 && rounds <= Q4_KEPT) {
+    float lo = (float)(Q4_SLOTS - items * p.Hkv) / fmaxf(all, 1.f), hi = (float)Q4_SLOTS / fmaxf(all, 1.f);      // fits; is too many
+    for (int i = 0; i < 5; ++i) {
+      const float mid = 0.5f * (lo + hi);
+      int n = 0;
+#pragma unroll
+      for (int c = 0; c < Q4_KEPT; ++c)
+        if (c < rounds) {
+          const Q4Count k = q4_count(sc, kept_blocks[c], kept_rows[c], mid);
+          n += kept_rows[c] / Q4_ROWS * k.full + k.tail;
+        }
+      if (wave_total(n) * p.Hkv <= Q4_SLOTS) lo = mid; else hi = mid;
+    }
+    density = lo;
+  }
   int base = 0, sbase = 0;
-  for (int c = 0; c < rounds; ++c) {
-    if (rounds > 1) load(c);
-    const int pf = q4_pieces(sc, cut.blocks, cut.full ? Q4_ROWS : 0, per_piece), pt = q4_pieces(sc, cut.blocks, cut.tail_rows, per_piece);
-    const int per_head = cut.full * pf + pt, split_head = cut.full * (pf > 1 ? pf : 0) + (pt > 1 ? pt : 0);
+  auto find = [&](int c, int blocks, int rows) FD_INLINE {
+    const Q4Count k = q4_count(sc, blocks, rows, density);
+    const int full = rows / Q4_ROWS, per_head = full * k.full + k.tail, split_head = full * (k.full > 1 ? k.full : 0) + (k.tail > 1 ? k.tail : 0);
     const int it = wave_incl_scan(p.Hkv * per_head), st = wave_incl_scan(p.Hkv * split_head);
     const int end = base + it, begin = end - p.Hkv * per_head;
     const unsigned long long here = __ballot(w >= begin && w < end);
     if (here) {
       const int l = __ffsll((long long)here) - 1;
-      auto from = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+      auto from = [&](int v) FD_INLINE { return __builtin_amdgcn_readlane(v, l); };
       int x = w - from(begin), sl = sbase + from(st - p.Hkv * split_head);
-      const int full = from(cut.full), f = from(pf), t = from(pt), ph = from(per_head);
+      const int fl = from(full), f = from(k.full), t = from(k.tail), ph = from(per_head);
       out.head = x / ph;
       x -= out.head * ph; sl += out.head * from(split_head);
-      if (x < full * f) { out.rt = x / f; x -= out.rt * f; out.pieces = f; sl += f > 1 ? out.rt * f : 0; }
-      else { out.rt = full; x -= full * f; out.pieces = t; sl += f > 1 ? full * f : 0; }
+      if (x < fl * f) { out.rt = x / f; x -= out.rt * f; out.pieces = f; sl += f > 1 ? out.rt * f : 0; }
+      else { out.rt = fl; x -= fl * f; out.pieces = t; sl += f > 1 ? fl * f : 0; }
       out.piece = x; out.slot = sl;
       out.item = ((c * 64 + l) * p.Hkv + out.head) * sc.rt_max + out.rt;
-      out.s = SeqInfo{from(mine.L), from(mine.row0), from(mine.n), from(mine.k), from(mine.v), from(mine.nb), from(mine.page0), from(mine.npages)};
+      out.s = load_seq(p, c * 64 + l);
       return true;
     }
     base += __builtin_amdgcn_readlane(it, 63);
     sbase += __builtin_amdgcn_readlane(st, 63);
+    return false;
+  };
+  bool found = false;
+#pragma unroll
+  for (int c = 0; c < Q4_KEPT; ++c)
+    if (!found && c < rounds) found = find(c, kept_blocks[c], kept_rows[c]);
+  for (int c = Q4_KEPT; c < rounds && !found; ++c) {
+    int blocks, rows;
+    load(c, blocks, rows);
+    found = find(c, blocks, rows);
   }
-  return false;
+  return found;
 }
 
 typedef __attribute__((ext_vector_type(8))) short s16x8;
@@ -119,6 +166,11 @@ __device__ __forceinline__ bf16x8 as_bf16x8(u32x4 x) { return __builtin_bit_cast
 __device__ __forceinline__ unsigned pack_bf16x2(float lo, float hi) {
   const f32x2 f = {lo, hi};
   return __builtin_bit_cast(unsigned, __builtin_convertvector(f, bf16x2));      // round to nearest even
+}
+__device__ __forceinline__ unsigned pack_f16x2(float lo, float hi) {
+  typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+  const f32x2 f = {lo, hi};
+  return __builtin_bit_cast(unsigned, __builtin_convertvector(f, f16x2));
 }
 // The larger of a lane's value and that of lane ^ 32.
 __device__ __forceinline__ float max_halves(float x) {
@@ -543,10 +595,23 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
     if (pc.pieces > 1) {
       if (pc.slot + pc.piece >= sc.max_partials) continue;           // (only where the device's rows contradict the host's bounds)
       const long long at = (long long)(pc.slot + pc.piece) * Q4_ROWS + r;
-      float* dst = sc.part_acc + at * DH + part * CPT;
+      float big = 0.f;
 #pragma unroll
-      for (int e = 0; e < CPT; e += 4) *reinterpret_cast<f32x4*>(dst + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
-      if (part == 0) *reinterpret_cast<float2*>(sc.part_ml + at * 2) = make_float2(M, sum);
+      for (int e = 0; e < CPT; ++e) big = fmaxf(big, fabsf(acc[e]));
+#pragma unroll
+      for (int d = 1; d < TPR; d <<= 1) big = fmaxf(big, __shfl_xor(big, d));
+      // fp16 relative to the row's largest magnitude: off by 2^-12 of it, where the result's own rounding is 2^-8 of its value.  A row with an infinity
+      // or a NaN (fmaxf does not see one) keeps both: they are their own fp16.  (A reciprocal that is no number: the row stays fp32's subnormals, zeros.)
+      const bool scaled = big > 1e-37f && big < INFINITY;
+      const float inv = scaled ? 1.f / big : 1.f;
+      unsigned* dst = reinterpret_cast<unsigned*>(sc.part_acc + at * DH + part * CPT);
+      u32x4 w;
+#pragma unroll
+      for (int e = 0; e < CPT; e += 2) {
+        w[e / 2 % 4] = pack_f16x2(acc[e] * inv, acc[e + 1] * inv);
+        if (e % 8 == 6) *reinterpret_cast<u32x4*>(dst + e / 8 * 4) = w;
+      }
+      if (part == 0) *reinterpret_cast<f32x4*>(sc.part_ml + at * 4) = f32x4{M, sum, scaled ? big : 1.f, 0.f};
     } else {
       const int t = pc.rt * Q4_ROWS + r, n = t / p.G;
       const long long orow = (long long)(s.row0 + n) * p.Hq + pc.head * p.G + (t - n * p.G);
@@ -561,11 +626,12 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
   }
 }
 
-// Merge of the partials of split items, by rows: a row is taken by TPR = DH / 8 lanes, eight channels each.  TPR pieces at a time: lane j
-// reads the maximum and sum of piece j, so that they are one latency, and the rows' values are requested four pieces at once.
+// Merge of the partials of split items, by rows: a row is taken by TPR = DH / 8 lanes, eight channels each.  AT_ONCE pieces at a time, lane j of them
+// knows the maximum and sum of piece j; their values are requested with those, so that a batch is one latency.
 template <int DH>
 __global__ __launch_bounds__(256) void attn_q4_combine_kernel(AttnParams p, Q4Sched sc) {
-  constexpr int TPR = DH / 8, RPB = 256 / TPR, AT_ONCE = 4;
+  typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+  constexpr int TPR = DH / 8, RPB = 256 / TPR, AT_ONCE = 8;
   const int item = blockIdx.x, rt = item % sc.rt_max, head = item / sc.rt_max % p.Hkv, seq = item / sc.rt_max / p.Hkv;
   const int2 e = sc.entries[item];
   // (a sequence without new rows, or with fewer, has no such item: what stands in its entry is old)
@@ -576,39 +642,36 @@ __global__ __launch_bounds__(256) void attn_q4_combine_kernel(AttnParams p, Q4Sc
   const int r = blockIdx.y * RPB + threadIdx.x / TPR, part = threadIdx.x % TPR;
   if ((int)blockIdx.y * RPB >= rows || pieces <= 1 || slot < 0 || (long long)slot + pieces > sc.max_partials) return;
   const int rr = r < rows ? r : 0;                       // (every lane takes part in the exchanges)
+  const int j = part % AT_ONCE, lane0 = (threadIdx.x & 63) / TPR * TPR;
   float M = -3e38f, sum = 0.f, acc[8] = {};
-  for (int q0 = 0; q0 < pieces; q0 += TPR) {
-    const int n = min(TPR, pieces - q0);
+  for (int q0 = 0; q0 < pieces; q0 += AT_ONCE) {
+    const int n = min(AT_ONCE, pieces - q0);
     const long long at = (long long)(slot + q0) * Q4_ROWS + rr;
-    float2 ml = make_float2(-3e38f, 0.f);
-    if (part < n) ml = *reinterpret_cast<const float2*>(sc.part_ml + (at + (long long)part * Q4_ROWS) * 2);
-    float top = ml.x;
+    f32x4 ml = {-3e38f, 0.f, 0.f, 0.f};
+    if (j < n) ml = *reinterpret_cast<const f32x4*>(sc.part_ml + (at + (long long)j * Q4_ROWS) * 4);
+    u32x4 w[AT_ONCE];
 #pragma unroll
-    for (int d = 1; d < TPR; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+    for (int u = 0; u < AT_ONCE; ++u) w[u] = *reinterpret_cast<const u32x4*>(sc.part_acc + (at + (long long)min(u, n - 1) * Q4_ROWS) * DH + part * 8);
+    float top = ml[0];
+#pragma unroll
+    for (int d = 1; d < AT_ONCE; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
     const float mn = fmaxf(M, top), shrink = __builtin_amdgcn_exp2f(M - mn);
-    const float f = __builtin_amdgcn_exp2f(ml.x - mn);   // this lane's piece
-    float add = f * ml.y;
+    const float f = __builtin_amdgcn_exp2f(ml[0] - mn);  // this lane's piece
+    float add = f * ml[1];
 #pragma unroll
-    for (int d = 1; d < TPR; d <<= 1) add += __shfl_xor(add, d);
+    for (int d = 1; d < AT_ONCE; d <<= 1) add += __shfl_xor(add, d);
+    const float weight = f * ml[2];
     M = mn;
     sum = sum * shrink + add;
 #pragma unroll
     for (int u = 0; u < 8; ++u) acc[u] *= shrink;
-    const float* src = sc.part_acc + at * DH + part * 8;
-    for (int q = 0; q < n; q += AT_ONCE) {
-      f32x4 x[AT_ONCE][2];
 #pragma unroll
-      for (int u = 0; u < AT_ONCE; ++u) {
-        const f32x4* y = reinterpret_cast<const f32x4*>(src + (long long)min(q + u, n - 1) * Q4_ROWS * DH);
-        x[u][0] = y[0]; x[u][1] = y[1];
-      }
+    for (int u = 0; u < AT_ONCE; ++u) {
+      if (u >= n) break;                                 // (uniform; no zero times an infinity)
+      const float g = __shfl(weight, lane0 + u);
+      const f16x8 v = __builtin_bit_cast(f16x8, w[u]);
 #pragma unroll
-      for (int u = 0; u < AT_ONCE; ++u) {
-        if (q + u >= n) break;                           // (uniform; no zero times an infinity)
-        const float w = __shfl(f, (int)(threadIdx.x & 63) / TPR * TPR + q + u);
-#pragma unroll
-        for (int v = 0; v < 4; ++v) { acc[v] += w * x[u][0][v]; acc[4 + v] += w * x[u][1][v]; }
-      }
+      for (int k = 0; k < 8; ++k) acc[k] += g * (float)v[k];
     }
   }
   if (r >= rows) return;
@@ -638,19 +701,20 @@ static Q4Shape q4_shape(int batch, int num_kv_heads, int group, int total_rows, 
   z.unit_shift = 0;
   while (units / (double)(1ll << z.unit_shift) >= 1073741824.0) ++z.unit_shift;
   if (z.fixed > 0) {
-    z.wgs = z.items * ((blocks + z.fixed - 1) / z.fixed);
+    z.wgs = z.items * (blocks / z.fixed + 1);
     z.partials = z.wgs;
   } else {
-    // pieces - 1 of an item stay below its weight x blocks / target, which sum to Q4_PIECES over all items
+    // pieces - 1 of an item are density x units at most, which sum to Q4_PIECES over all items (Q4_SLOTS in one round)
+    static_assert(Q4_SLOTS <= Q4_PIECES, "what one round takes is within the bounds of several");
     z.wgs = z.items + Q4_PIECES;
     z.partials = 2 * Q4_PIECES;                                         // an item in c >= 2 pieces: c <= 2 (c - 1)
-    const long long most = z.items * ((blocks + Q4_MIN_PIECE - 1) / Q4_MIN_PIECE);
+    const long long most = z.items * (blocks / Q4_MIN_PIECE + 1);
     if (most < z.wgs) z.wgs = most;
     if (most < z.partials) z.partials = most;
   }
   auto round = [](size_t x) { return (x + 255) / 256 * 256; };
-  z.off_ml = round((size_t)z.partials * Q4_ROWS * head_dim * sizeof(float));
-  z.off_entries = z.off_ml + round((size_t)z.partials * Q4_ROWS * 2 * sizeof(float));
+  z.off_ml = round((size_t)z.partials * Q4_ROWS * head_dim * sizeof(unsigned short));
+  z.off_entries = z.off_ml + round((size_t)z.partials * Q4_ROWS * 4 * sizeof(float));
   z.total = z.off_entries + round((size_t)(batch > 0 ? batch : 1) * num_kv_heads * z.rt_max * sizeof(int2));
   return z;
 }
@@ -665,7 +729,7 @@ size_t attn_q4_workspace(int batch, int num_kv_heads, int group, int total_rows,
 hipError_t run_attn_q4(const AttnParams& p, const Q4Cache& c, void* workspace, int kv_chunk, hipStream_t st) {
   const Q4Shape z = q4_shape(p.B, p.Hkv, p.G, p.total_rows, p.max_kv_len, p.max_new_rows, kv_chunk, p.D);
   char* ws = reinterpret_cast<char*>(workspace);
-  const Q4Sched sc = {z.fixed, z.unit_shift, z.rt_max, (int)z.partials, reinterpret_cast<float*>(ws), reinterpret_cast<float*>(ws + z.off_ml), reinterpret_cast<int2*>(ws + z.off_entries)};
+  const Q4Sched sc = {z.fixed, z.fixed > 0 ? 1.f / (float)z.fixed : 0.f, z.unit_shift, z.rt_max, (int)z.partials, reinterpret_cast<unsigned short*>(ws), reinterpret_cast<float*>(ws + z.off_ml), reinterpret_cast<int2*>(ws + z.off_entries)};
   if (z.wgs == 0) return hipSuccess;
   const int per_row = p.D / 8, most_rows = (int)((long long)p.max_new_rows * p.G < Q4_ROWS ? p.max_new_rows * p.G : Q4_ROWS);
   const dim3 grid((unsigned)((long long)p.B * p.Hkv * z.rt_max), (most_rows * per_row + 255) / 256);

@@ -82,11 +82,14 @@ class Q4Call:
         torch.cuda.synchronize()
         return self.out.float().cpu().numpy().astype(np.float64), self.lse.cpu().numpy().astype(np.float64)
 
-    def oracle(self, sm_scale=None, magnitudes=False):
+    def oracle(self, sm_scale=None, magnitudes=False, peaks=False):
+        """magnitudes: with |v| for v; peaks: with the largest |v| of its token and head in the place of every channel."""
         k, v = self.cache.key_values(), self.cache.value_values()
         v_new = oa.widen_bf16(self.v_new)
         R = int(self.n.sum())
         f = np.abs if magnitudes else (lambda x: x)
+        if peaks:
+            f = lambda x: np.broadcast_to(np.abs(x).max(-1, keepdims=True), x.shape)  # noqa: E731
         return oa.verify_draft_attention(self.q[:R], self.k_new[:R], f(v_new[:R]), np.nan_to_num(k, nan=0.0), f(np.nan_to_num(v, nan=0.0)), self.page_indptr,
                                          self.page_indices, self.kv, self.row_indptr, self.k, self.vis, self.blocks, page_size=self.ps, sm_scale=sm_scale)
 
@@ -94,17 +97,20 @@ class Q4Call:
         """The bounds.  A probability (times its value's scale) and the result are each rounded to bf16: half a step is 2^-8 of the value, so
         2^-8 (|o| + sum p |v|) in all.  In fp32: a score sums D = 128 products in order, off by at most 128 * 2^-24 sum |q_d k_d| scale, which
         is below 2^-17 B with B the largest such sum; the base-2 exponential and the scales add 2^-22 of a probability each; the sum of n probabilities n * 2^-24.
-        A score that is off by x changes a probability, against the others, by at most 2 x of itself."""
+        A score that is off by x changes a probability, against the others, by at most 2 x of itself.
+        An item in several pieces leaves each piece's row as fp16 numbers over the row's largest entry: off by half a step of [1/2, 1), 2^-12 of that
+        entry, which is at most the piece's sum of p max |v|; over all pieces 2^-12 of the whole sum, and fp32 beside it."""
         R = int(self.n.sum())
         ref, ref_lse = self.oracle(sm_scale)
         size, _ = self.oracle(sm_scale, magnitudes=True)
+        peak, _ = self.oracle(sm_scale, peaks=True)
         D = self.q.shape[2]
         q, scale = np.abs(oa.widen_bf16(self.q[:R])), sm_scale or 1 / np.sqrt(D)
         kmax = max(np.abs(np.nan_to_num(self.cache.key_values())).max(), np.abs(oa.widen_bf16(self.k_new[:R])).max())
         score = 2.0 ** -17 * float(q.sum(-1).max() * kmax * scale) + 2.0 ** -20
         keys = self.max_kv + self.max_n
         assert np.isfinite(out[:R]).all() and np.isfinite(lse[:R]).all()
-        bound = 2.0 ** -8 * (np.abs(ref) + size) + (2 * score + keys * 2.0 ** -23) * size + 1e-30
+        bound = 2.0 ** -8 * (np.abs(ref) + size) + (2 * score + keys * 2.0 ** -23) * size + 2.0 ** -12 * (1 + 2.0 ** -8) * peak + 1e-30
         worst = float((np.abs(out[:R] - ref) / bound).max())
         assert worst <= 1.0, f"{worst:.2f} of the bound"
         off = np.abs(lse[:R] - ref_lse).max()
