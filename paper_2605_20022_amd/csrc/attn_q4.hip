@@ -74,56 +74,58 @@ struct Q4Piece { int head, rt, piece, pieces, slot, item; SeqInfo s; };
 __device__ __forceinline__ bool q4_find(const AttnParams& p, const Q4Sched& sc, int w, Q4Piece& out) {
   const int lane = threadIdx.x & 63;
   const int rounds = (p.B + 63) / 64;
-  int kept_blocks[Q4_KEPT], kept_rows[Q4_KEPT];
-  auto load = [&](int c, int& blocks, int& rows) FD_INLINE {
+  SeqInfo kept[Q4_KEPT];
+  auto load = [&](int c) FD_INLINE {
+    SeqInfo s = {};
     uint32_t bad = 0;
     const int i = c * 64 + lane;
-    blocks = rows = 0;
-    if (i < p.B) {
-      const SeqInfo s = load_seq_t<false>(p, i, &bad);
-      blocks = q4_blocks(s);
-      rows = s.n * p.G;
-    }
+    if (i < p.B) s = load_seq_t<false>(p, i, &bad);
     if (bad && w == 0 && threadIdx.x < 64) flag_status(p.status, bad);        // (work-group 0 comes by every sequence)
+    return s;
   };
   int total = 0, items = 0;                              // units of one head, in 2^unit_shift (the host's bounds say that they fit), and items
-  auto add = [&](int blocks, int rows) FD_INLINE {
+  auto add = [&](const SeqInfo& s) FD_INLINE {
+    const int blocks = q4_blocks(s), rows = s.n * p.G;
     // (rounded up, so that there are never more pieces than the host counts on)
     total += wave_total((int)((q4_units(blocks, rows) + (1ll << sc.unit_shift) - 1) >> sc.unit_shift));
     items += wave_total((rows + Q4_ROWS - 1) / Q4_ROWS);
   };
 #pragma unroll
   for (int c = 0; c < Q4_KEPT; ++c) {
-    kept_blocks[c] = kept_rows[c] = 0;
-    if (c < rounds) load(c, kept_blocks[c], kept_rows[c]);
+    kept[c] = SeqInfo{};
+    if (c < rounds) kept[c] = load(c);
   }
 #pragma unroll
   for (int c = 0; c < Q4_KEPT; ++c)
-    if (c < rounds) add(kept_blocks[c], kept_rows[c]);
-  for (int c = Q4_KEPT; c < rounds; ++c) {
-    int blocks, rows;
-    load(c, blocks, rows);
-    add(blocks, rows);
-  }
+    if (c < rounds) add(kept[c]);
+  for (int c = Q4_KEPT; c < rounds; ++c) add(load(c));
   const float all = ldexpf((float)total, sc.unit_shift) * (float)p.Hkv * 1.000001f;
   float density = (float)Q4_PIECES / fmaxf(all, 1.f);
   if (sc.fixed <= 0 && items * (long long)p.Hkv <= Q4_SLOTS / 2 && rounds <= Q4_KEPT) {
-    float lo = (float)(Q4_SLOTS - items * p.Hkv) / fmaxf(all, 1.f), hi = (float)Q4_SLOTS / fmaxf(all, 1.f);      // fits; is too many
-    for (int i = 0; i < 5; ++i) {
-      const float mid = 0.5f * (lo + hi);
+    auto fits = [&](float density) FD_INLINE {
       int n = 0;
 #pragma unroll
       for (int c = 0; c < Q4_KEPT; ++c)
         if (c < rounds) {
-          const Q4Count k = q4_count(sc, kept_blocks[c], kept_rows[c], mid);
-          n += kept_rows[c] / Q4_ROWS * k.full + k.tail;
+          const int rows = kept[c].n * p.G;
+          const Q4Count k = q4_count(sc, q4_blocks(kept[c]), rows, density);
+          n += rows / Q4_ROWS * k.full + k.tail;
         }
-      if (wave_total(n) * p.Hkv <= Q4_SLOTS) lo = mid; else hi = mid;
+      return wave_total(n) * p.Hkv <= Q4_SLOTS;
+    };
+    if (fits(1.f)) density = 1.f;                        // (pieces of Q4_MIN_PIECE blocks)
+    else {
+      float lo = (float)(Q4_SLOTS - items * p.Hkv) / all, hi = (float)Q4_SLOTS / all;      // fits; is too many
+      for (int i = 0; i < 4; ++i) {
+        const float mid = 0.5f * (lo + hi);
+        if (fits(mid)) lo = mid; else hi = mid;
+      }
+      density = lo;
     }
-    density = lo;
   }
   int base = 0, sbase = 0;
-  auto find = [&](int c, int blocks, int rows) FD_INLINE {
+  auto find = [&](int c, const SeqInfo& s) FD_INLINE {
+    const int blocks = q4_blocks(s), rows = s.n * p.G;
     const Q4Count k = q4_count(sc, blocks, rows, density);
     const int full = rows / Q4_ROWS, per_head = full * k.full + k.tail, split_head = full * (k.full > 1 ? k.full : 0) + (k.tail > 1 ? k.tail : 0);
     const int it = wave_incl_scan(p.Hkv * per_head), st = wave_incl_scan(p.Hkv * split_head);
@@ -140,7 +142,7 @@ __device__ __forceinline__ bool q4_find(const AttnParams& p, const Q4Sched& sc, 
       else { out.rt = fl; x -= fl * f; out.pieces = t; sl += f > 1 ? fl * f : 0; }
       out.piece = x; out.slot = sl;
       out.item = ((c * 64 + l) * p.Hkv + out.head) * sc.rt_max + out.rt;
-      out.s = load_seq(p, c * 64 + l);
+      out.s = SeqInfo{from(s.L), from(s.row0), from(s.n), from(s.k), from(s.v), from(s.nb), from(s.page0), from(s.npages)};
       return true;
     }
     base += __builtin_amdgcn_readlane(it, 63);
@@ -150,12 +152,8 @@ __device__ __forceinline__ bool q4_find(const AttnParams& p, const Q4Sched& sc, 
   bool found = false;
 #pragma unroll
   for (int c = 0; c < Q4_KEPT; ++c)
-    if (!found && c < rounds) found = find(c, kept_blocks[c], kept_rows[c]);
-  for (int c = Q4_KEPT; c < rounds && !found; ++c) {
-    int blocks, rows;
-    load(c, blocks, rows);
-    found = find(c, blocks, rows);
-  }
+    if (!found && c < rounds) found = find(c, kept[c]);
+  for (int c = Q4_KEPT; c < rounds && !found; ++c) found = find(c, load(c));
   return found;
 }
 
