@@ -25,7 +25,7 @@ constexpr int Q4_TK = 32;                 // keys of a block
 constexpr int Q4_ROWS = 128;              // tile rows of an item
 constexpr float Q4_LAZY = 256.f;          // sum of a row's sixteen probabilities from which on the softmax reference follows the row maximum
 constexpr int Q4_SLOTS = 512;             // work-groups that run at once: two a compute unit
-constexpr int Q4_PIECES = 1024;           // pieces aimed at where there are more than Q4_SLOTS / 2 items
+constexpr int Q4_PIECES = 768;            // pieces aimed at where there are more than Q4_SLOTS / 2 items
 constexpr int Q4_MIN_PIECE = 8;           // blocks of a piece, at least (but for the last of a short item)
 constexpr int Q4_KEPT = 4;                // rounds of 64 sequences whose lengths a wave keeps in registers
 
@@ -704,8 +704,10 @@ static Q4Shape q4_shape(int batch, int num_kv_heads, int group, int total_rows, 
   } else {
     // pieces - 1 of an item are density x units at most, which sum to Q4_PIECES over all items (Q4_SLOTS in one round)
     static_assert(Q4_SLOTS <= Q4_PIECES, "what one round takes is within the bounds of several");
-    z.wgs = z.items + Q4_PIECES;
-    z.partials = 2 * Q4_PIECES;                                         // an item in c >= 2 pieces: c <= 2 (c - 1)
+    // (work-groups without a piece are not free, 0.8 us for 528 of them: none where one round is sure to do)
+    const bool one_round = z.items <= Q4_SLOTS / 2 && batch <= 64 * Q4_KEPT;
+    z.wgs = one_round ? Q4_SLOTS : z.items + Q4_PIECES;
+    z.partials = one_round ? Q4_SLOTS : 2 * Q4_PIECES;                  // an item in c >= 2 pieces: c <= 2 (c - 1)
     const long long most = z.items * (blocks / Q4_MIN_PIECE + 1);
     if (most < z.wgs) z.wgs = most;
     if (most < z.partials) z.partials = most;
