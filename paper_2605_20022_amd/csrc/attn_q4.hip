@@ -25,9 +25,10 @@ constexpr int Q4_TK = 32;                 // keys of a block
 constexpr int Q4_ROWS = 128;              // tile rows of an item
 constexpr float Q4_LAZY = 256.f;          // sum of a row's sixteen probabilities from which on the softmax reference follows the row maximum
 constexpr int Q4_SLOTS = 512;             // work-groups that run at once: two a compute unit
-constexpr int Q4_PIECES = 768;            // pieces aimed at where there are more than Q4_SLOTS / 2 items
+constexpr int Q4_PIECES = 512;            // pieces aimed at where there are more than Q4_SLOTS / 2 items
+constexpr int Q4_CLASSES = 4;             // lengths of pieces that are told apart
 constexpr int Q4_MIN_PIECE = 8;           // blocks of a piece, at least (but for the last of a short item)
-constexpr int Q4_KEPT = 4;                // rounds of 64 sequences whose lengths a wave keeps in registers
+constexpr int Q4_KEPT = 4;                // rounds of 64 sequences whose lengths a wave keeps in LDS
 
 struct Q4Sched {
   int fixed;                // > 0: blocks of a piece, asked for by the caller
@@ -63,18 +64,38 @@ __device__ __forceinline__ Q4Count q4_count(const Q4Sched& sc, int blocks, int r
   return Q4Count{rows >= Q4_ROWS ? q4_pieces(sc, blocks, Q4_ROWS, density) : 0, q4_pieces(sc, blocks, rows % Q4_ROWS, density)};
 }
 
+// How long a sequence's longest piece takes a work-group, in units.
+__device__ __forceinline__ int q4_longest(const Q4Sched& sc, int blocks, int rows, float density) {
+  const int r = min(rows, Q4_ROWS);
+  return rows > 0 ? (int)((float)blocks * (float)q4_weight(r) / (float)q4_pieces(sc, blocks, r, density)) : 0;
+}
+
 struct Q4Piece { int head, rt, piece, pieces, slot, item; SeqInfo s; };
 
-// Which piece work-group w takes: pieces are numbered by (sequence, head, item, piece).  Every wave finds it by itself, a sequence a lane, 64 at a
-// time: the lengths are one latency of memory, the rest lane shifts, and no wave waits for another.  false: none.
+__device__ __forceinline__ int wave_max(int v) {         // of values >= 0
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));
+  return __builtin_amdgcn_readlane(v, 63);
+}
+
+// Which piece work-group w takes: pieces are numbered by (class, sequence, head, item, piece).  Every wave finds it by itself, a sequence a lane, 64 at
+// a time: the lengths are one latency of memory, the rest LDS of its own and lane shifts, and no wave waits for another.  false: none.
 //
 // How many pieces: with at most Q4_SLOTS / 2 items as many as run at once, found by bisection, so that one round does it: a piece's start and
 // end cost about as much as twelve blocks (find, pages, first codes, merge), and a second round would wait for the first.  Else Q4_PIECES and
-// the items themselves, dealt out as work-groups become free.
-__device__ __forceinline__ bool q4_find(const AttnParams& p, const Q4Sched& sc, int w, Q4Piece& out) {
+// the items themselves, dealt out as work-groups become free, the sequences with the longest pieces first: one that began last would be waited for
+// (128 sequences of 1024 to 8192 keys: 170 us, in the order of the batch 200; 512 pieces and items 170, 640 176, 768 177).
+//
+// FEW (up to 64 sequences): lengths stay in registers.  Without it the same calls take 0.5 to 1.6 us longer, with its code for more rounds unrolled as much.
+template <bool FEW>
+__device__ __forceinline__ bool q4_find(const AttnParams& p, const Q4Sched& sc, int w, int4* kept, Q4Piece& out) {
   const int lane = threadIdx.x & 63;
-  const int rounds = (p.B + 63) / 64;
-  SeqInfo kept[Q4_KEPT];
+  const int rounds = FEW ? 1 : (p.B + 63) / 64;
+  SeqInfo only = {};
   auto load = [&](int c) FD_INLINE {
     SeqInfo s = {};
     uint32_t bad = 0;
@@ -83,78 +104,98 @@ __device__ __forceinline__ bool q4_find(const AttnParams& p, const Q4Sched& sc, 
     if (bad && w == 0 && threadIdx.x < 64) flag_status(p.status, bad);        // (work-group 0 comes by every sequence)
     return s;
   };
-  int total = 0, items = 0;                              // units of one head, in 2^unit_shift (the host's bounds say that they fit), and items
-  auto add = [&](const SeqInfo& s) FD_INLINE {
-    const int blocks = q4_blocks(s), rows = s.n * p.G;
-    // (rounded up, so that there are never more pieces than the host counts on)
-    total += wave_total((int)((q4_units(blocks, rows) + (1ll << sc.unit_shift) - 1) >> sc.unit_shift));
-    items += wave_total((rows + Q4_ROWS - 1) / Q4_ROWS);
+  auto get = [&](int c, int l) FD_INLINE {               // the round's l-th sequence
+    if (FEW) return only;
+    if (c >= Q4_KEPT) return load(c);
+    const int4 a = kept[(c * 2) * 64 + l], b = kept[(c * 2 + 1) * 64 + l];
+    return SeqInfo{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
   };
-#pragma unroll
-  for (int c = 0; c < Q4_KEPT; ++c) {
-    kept[c] = SeqInfo{};
-    if (c < rounds) kept[c] = load(c);
+  int total = 0, items = 0;                              // units of one head, in 2^unit_shift (the host's bounds say that they fit), and items
+#pragma unroll 1
+  for (int c = 0; c < rounds; ++c) {
+    const SeqInfo s = load(c);
+    if (FEW) only = s;
+    else if (c < Q4_KEPT) {
+      kept[(c * 2) * 64 + lane] = make_int4(s.L, s.row0, s.n, s.k);
+      kept[(c * 2 + 1) * 64 + lane] = make_int4(s.v, s.nb, s.page0, s.npages);
+    }
+    const int rows = s.n * p.G;
+    // (rounded up, so that there are never more pieces than the host counts on)
+    total += wave_total((int)((q4_units(q4_blocks(s), rows) + (1ll << sc.unit_shift) - 1) >> sc.unit_shift));
+    items += wave_total((rows + Q4_ROWS - 1) / Q4_ROWS);
   }
-#pragma unroll
-  for (int c = 0; c < Q4_KEPT; ++c)
-    if (c < rounds) add(kept[c]);
-  for (int c = Q4_KEPT; c < rounds; ++c) add(load(c));
   const float all = ldexpf((float)total, sc.unit_shift) * (float)p.Hkv * 1.000001f;
   float density = (float)Q4_PIECES / fmaxf(all, 1.f);
-  if (sc.fixed <= 0 && items * (long long)p.Hkv <= Q4_SLOTS / 2 && rounds <= Q4_KEPT) {
-    auto fits = [&](float density) FD_INLINE {
-      int n = 0;
-#pragma unroll
-      for (int c = 0; c < Q4_KEPT; ++c)
-        if (c < rounds) {
-          const int rows = kept[c].n * p.G;
-          const Q4Count k = q4_count(sc, q4_blocks(kept[c]), rows, density);
+  int classes = 1;
+  float part = 0.f;                                      // classes a unit of time
+  if (sc.fixed <= 0 && rounds <= Q4_KEPT) {
+    if (items * (long long)p.Hkv <= Q4_SLOTS / 2) {
+      // first whether pieces of Q4_MIN_PIECE blocks fit, then between what fits and what is too many
+      float lo = (float)(Q4_SLOTS - items * p.Hkv) / fmaxf(all, 1.f), hi = (float)Q4_SLOTS / fmaxf(all, 1.f);
+      density = 1.f;
+#pragma unroll 1
+      for (int i = 0; i < 5; ++i) {
+        int n = 0;
+#pragma unroll 1
+        for (int c = 0; c < rounds; ++c) {
+          const SeqInfo s = get(c, lane);
+          const int rows = s.n * p.G;
+          const Q4Count k = q4_count(sc, q4_blocks(s), rows, density);
           n += rows / Q4_ROWS * k.full + k.tail;
         }
-      return wave_total(n) * p.Hkv <= Q4_SLOTS;
-    };
-    if (fits(1.f)) density = 1.f;                        // (pieces of Q4_MIN_PIECE blocks)
-    else {
-      float lo = (float)(Q4_SLOTS - items * p.Hkv) / all, hi = (float)Q4_SLOTS / all;      // fits; is too many
-      for (int i = 0; i < 4; ++i) {
-        const float mid = 0.5f * (lo + hi);
-        if (fits(mid)) lo = mid; else hi = mid;
+        const bool fits = wave_total(n) * p.Hkv <= Q4_SLOTS;
+        if (i == 0) { if (fits) { lo = density; break; } }
+        else if (fits) lo = density;
+        else hi = density;
+        density = 0.5f * (lo + hi);
       }
       density = lo;
+    } else {
+      int top = 1;
+#pragma unroll 1
+      for (int c = 0; c < rounds; ++c) {
+        const SeqInfo s = get(c, lane);
+        top = max(top, q4_longest(sc, q4_blocks(s), s.n * p.G, density));
+      }
+      classes = Q4_CLASSES;
+      part = (float)Q4_CLASSES / (float)wave_max(top);
     }
   }
   int base = 0, sbase = 0;
-  auto find = [&](int c, const SeqInfo& s) FD_INLINE {
-    const int blocks = q4_blocks(s), rows = s.n * p.G;
-    const Q4Count k = q4_count(sc, blocks, rows, density);
-    const int full = rows / Q4_ROWS, per_head = full * k.full + k.tail, split_head = full * (k.full > 1 ? k.full : 0) + (k.tail > 1 ? k.tail : 0);
-    const int it = wave_incl_scan(p.Hkv * per_head), st = wave_incl_scan(p.Hkv * split_head);
-    const int end = base + it, begin = end - p.Hkv * per_head;
-    const unsigned long long here = __ballot(w >= begin && w < end);
-    if (here) {
-      const int l = __ffsll((long long)here) - 1;
-      auto from = [&](int v) FD_INLINE { return __builtin_amdgcn_readlane(v, l); };
-      int x = w - from(begin), sl = sbase + from(st - p.Hkv * split_head);
-      const int fl = from(full), f = from(k.full), t = from(k.tail), ph = from(per_head);
-      out.head = x / ph;
-      x -= out.head * ph; sl += out.head * from(split_head);
-      if (x < fl * f) { out.rt = x / f; x -= out.rt * f; out.pieces = f; sl += f > 1 ? out.rt * f : 0; }
-      else { out.rt = fl; x -= fl * f; out.pieces = t; sl += f > 1 ? fl * f : 0; }
-      out.piece = x; out.slot = sl;
-      out.item = ((c * 64 + l) * p.Hkv + out.head) * sc.rt_max + out.rt;
-      out.s = SeqInfo{from(s.L), from(s.row0), from(s.n), from(s.k), from(s.v), from(s.nb), from(s.page0), from(s.npages)};
-      return true;
+#pragma unroll 1
+  for (int turn = 0; turn < classes; ++turn)
+#pragma unroll 1
+    for (int c = 0; c < rounds; ++c) {
+      const SeqInfo s = get(c, lane);
+      const int blocks = q4_blocks(s);
+      int rows = s.n * p.G;
+      if (classes > 1) {
+        if (Q4_CLASSES - 1 - min((int)((float)q4_longest(sc, blocks, rows, density) * part), Q4_CLASSES - 1) != turn) rows = 0;
+        if (__ballot(rows > 0) == 0) continue;
+      }
+      const Q4Count k = q4_count(sc, blocks, rows, density);
+      const int full = rows / Q4_ROWS, per_head = full * k.full + k.tail, split_head = full * (k.full > 1 ? k.full : 0) + (k.tail > 1 ? k.tail : 0);
+      const int it = wave_incl_scan(p.Hkv * per_head), st = wave_incl_scan(p.Hkv * split_head);
+      const int end = base + it, begin = end - p.Hkv * per_head;
+      const unsigned long long here = __ballot(w >= begin && w < end);
+      if (here) {
+        const int l = __ffsll((long long)here) - 1;
+        auto from = [&](int v) FD_INLINE { return __builtin_amdgcn_readlane(v, l); };
+        int x = w - from(begin), sl = sbase + from(st - p.Hkv * split_head);
+        const int fl = from(full), f = from(k.full), t = from(k.tail), ph = from(per_head);
+        out.head = x / ph;
+        x -= out.head * ph; sl += out.head * from(split_head);
+        if (x < fl * f) { out.rt = x / f; x -= out.rt * f; out.pieces = f; sl += f > 1 ? out.rt * f : 0; }
+        else { out.rt = fl; x -= fl * f; out.pieces = t; sl += f > 1 ? fl * f : 0; }
+        out.piece = x; out.slot = sl;
+        out.item = ((c * 64 + l) * p.Hkv + out.head) * sc.rt_max + out.rt;
+        out.s = SeqInfo{from(s.L), from(s.row0), from(s.n), from(s.k), from(s.v), from(s.nb), from(s.page0), from(s.npages)};
+        return true;
+      }
+      base += __builtin_amdgcn_readlane(it, 63);
+      sbase += __builtin_amdgcn_readlane(st, 63);
     }
-    base += __builtin_amdgcn_readlane(it, 63);
-    sbase += __builtin_amdgcn_readlane(st, 63);
-    return false;
-  };
-  bool found = false;
-#pragma unroll
-  for (int c = 0; c < Q4_KEPT; ++c)
-    if (!found && c < rounds) found = find(c, kept[c]);
-  for (int c = Q4_KEPT; c < rounds && !found; ++c) found = find(c, load(c));
-  return found;
+  return false;
 }
 
 typedef __attribute__((ext_vector_type(8))) short s16x8;
@@ -200,7 +241,7 @@ template <int DH> struct Q4Values {
   u32x4 scale[2];            // the scales of those eight keys
 };
 
-template <int DH>
+template <int DH, bool FEW>
 __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Cache c, Q4Sched sc) {
   constexpr int NA = DH / 64, NC = DH / 32, STEPS = DH / 16;
   constexpr int OP = DH + 4;                             // pitch of an O row in LDS, floats: an odd number of 16-byte slots
@@ -209,7 +250,8 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l31 = lane & 31, h = lane >> 5;
   Q4Piece pc;
-  if (!q4_find(p, sc, blockIdx.x, pc)) return;
+  static_assert(Q4_KEPT * 2 * 64 * sizeof(int4) <= sizeof(lds_o[0]), "the lengths fit a wave's part of LDS");
+  if (!q4_find<FEW>(p, sc, blockIdx.x, reinterpret_cast<int4*>(&lds_o[wave][0][0]), pc)) return;
   const SeqInfo& s = pc.s;
   const int rows = min(Q4_ROWS, s.n * p.G - pc.rt * Q4_ROWS);
   const int RB = q4_row_blocks(rows), ks_shift = RB == 1 ? 2 : RB == 2 ? 1 : 0, KS = 1 << ks_shift;
@@ -734,10 +776,12 @@ hipError_t run_attn_q4(const AttnParams& p, const Q4Cache& c, void* workspace, i
   const int per_row = p.D / 8, most_rows = (int)((long long)p.max_new_rows * p.G < Q4_ROWS ? p.max_new_rows * p.G : Q4_ROWS);
   const dim3 grid((unsigned)((long long)p.B * p.Hkv * z.rt_max), (most_rows * per_row + 255) / 256);
   if (p.D == 128) {
-    hipLaunchKernelGGL(attn_q4_kernel<128>, dim3((unsigned)z.wgs), dim3(Q4_BLOCK), 0, st, p, c, sc);
+    if (p.B <= 64) hipLaunchKernelGGL((attn_q4_kernel<128, true>), dim3((unsigned)z.wgs), dim3(Q4_BLOCK), 0, st, p, c, sc);
+    else hipLaunchKernelGGL((attn_q4_kernel<128, false>), dim3((unsigned)z.wgs), dim3(Q4_BLOCK), 0, st, p, c, sc);
     hipLaunchKernelGGL(attn_q4_combine_kernel<128>, grid, dim3(256), 0, st, p, sc);
   } else {
-    hipLaunchKernelGGL(attn_q4_kernel<64>, dim3((unsigned)z.wgs), dim3(Q4_BLOCK), 0, st, p, c, sc);
+    if (p.B <= 64) hipLaunchKernelGGL((attn_q4_kernel<64, true>), dim3((unsigned)z.wgs), dim3(Q4_BLOCK), 0, st, p, c, sc);
+    else hipLaunchKernelGGL((attn_q4_kernel<64, false>), dim3((unsigned)z.wgs), dim3(Q4_BLOCK), 0, st, p, c, sc);
     hipLaunchKernelGGL(attn_q4_combine_kernel<64>, grid, dim3(256), 0, st, p, sc);
   }
   return hipGetLastError();
