@@ -383,9 +383,9 @@ FD_API fd_status fd_step_tables(const fd_table_args *args, void *hip_stream);
  * num_kv_heads heads that are copied as they are.
  */
 typedef struct fd_rope_args {
-  int32_t total_rows;         /* R >= 0                                                       */
-  int32_t num_q_heads;        /* >= 0                                                         */
-  int32_t num_kv_heads;       /* >= 0                                                         */
+  int32_t total_rows;         /* R in [0, 2^25]                                               */
+  int32_t num_q_heads;        /* [0, 4096]                                                    */
+  int32_t num_kv_heads;       /* [0, 4096]                                                    */
   int32_t head_dim;           /* D: multiple of 8, <= 256                                     */
   int32_t rotary_dim;         /* multiple of 8 in [0, D]                                      */
   int32_t interleaved;        /* pairs side by side instead of half a rotary_dim apart        */

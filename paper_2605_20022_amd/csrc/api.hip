@@ -506,6 +506,7 @@ fd_status fd_qk_norm_rope(const fd_rope_args* a, void* hip_stream) {
     return fail(FD_ERR_INVALID_ARG, "rotary_dim %d must be a multiple of 8 from 0 to head_dim %d", a->rotary_dim, a->head_dim);
   if (a->dtype != FD_F32 && a->dtype != FD_BF16) return fail(FD_ERR_INVALID_ARG, "unknown dtype %d", a->dtype);
   if (!(a->eps >= 0.f) || isinf(a->eps)) return fail(FD_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  if (a->total_rows > (1 << 25)) return fail(FD_ERR_UNSUPPORTED, "total_rows %d > 2^25", a->total_rows);       // (four rows a work-group of 256)
   if (a->num_q_heads > 4096 || a->num_kv_heads > 4096) return fail(FD_ERR_UNSUPPORTED, "%d / %d heads > 4096", a->num_q_heads, a->num_kv_heads);
   g_err[0] = 0;
   if (a->total_rows == 0 || a->num_q_heads + a->num_kv_heads == 0) return FD_OK;

@@ -761,10 +761,10 @@ static Q4Shape q4_shape(int batch, int num_kv_heads, int group, int total_rows, 
   return z;
 }
 
-// 0 where the call is too large for one launch.
+// 0 where the call is too large for one launch (2^24 work-groups of 256 threads).
 size_t attn_q4_workspace(int batch, int num_kv_heads, int group, int total_rows, int max_kv_len, int max_new_rows, int kv_chunk, int head_dim) {
   const Q4Shape z = q4_shape(batch, num_kv_heads, group, total_rows, max_kv_len, max_new_rows, kv_chunk, head_dim);
-  if (z.wgs >= (1ll << 31) || (long long)batch * num_kv_heads * z.rt_max >= (1ll << 31)) return 0;
+  if (z.wgs >= (1ll << 24) || (long long)batch * num_kv_heads * z.rt_max >= (1ll << 24)) return 0;
   return z.total > 0 ? z.total : 256;
 }
 

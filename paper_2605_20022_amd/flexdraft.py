@@ -41,6 +41,7 @@ class fd_attn_args(C.Structure):
         ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
         ("status", C.c_void_p),
     ]
+    device, cache = -1, None     # of make_attn_args_q4: where the tensors are whose addresses these are, and the cache in 4 bits
 
 
 class fd_table_args(C.Structure):
@@ -53,6 +54,7 @@ class fd_table_args(C.Structure):
         ("row_indptr", C.c_void_p), ("page_indptr", C.c_void_p), ("page_indices", C.c_void_p),
         ("positions", C.c_void_p), ("slot_map", C.c_void_p), ("status", C.c_void_p),
     ]
+    device = -1                  # where the tensors are whose addresses these are
 
 
 class fd_rope_args(C.Structure):
@@ -317,6 +319,26 @@ def _opt_i32(t: Optional[torch.Tensor], name: str):
     return None if t is None else _i32(t, name).data_ptr()
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _one_device(*tensors: Optional[torch.Tensor]) -> int:
+    """The index of the device on which all of them are, -1 for the CPU."""
+    device = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise TypeError("the tensors are on different devices")
+    return device
+
+
+def _launchable(device: int) -> None:
+    """A kernel runs on the current device, and what it is given has to be there."""
+    if device < 0:
+        raise TypeError("the tensors are on the CPU")
+    if device != _current_device():
+        raise TypeError(f"the tensors are on device {device}, the current device is {_current_device()}")
+
+
 def make_table_args(kv_len, verify_len, block_table, table_len, free_pages, free_count, mask_rows=None, mask_vis=None, mask_blocks=None, *,
                     page_size: int, row_indptr, page_indptr, page_indices, positions=None, slot_map=None, table_len_out=None,
                     free_count_out=None, status=None):
@@ -334,6 +356,8 @@ def make_table_args(kv_len, verify_len, block_table, table_len, free_pages, free
         raise TypeError("slot_map must be a contiguous int64 tensor")
     rows = [t.numel() for t in (positions, slot_map) if t is not None]
     a = fd_table_args()
+    a.device = _one_device(kv_len, verify_len, block_table, table_len, free_pages, free_count, mask_rows, mask_vis, mask_blocks, row_indptr, page_indptr,
+                           page_indices, positions, slot_map, table_len_out, free_count_out, status)
     a.batch = B; a.page_size = int(page_size); a.table_stride = block_table.shape[1]
     # without positions and slots there is nothing to bound the rows by but the call's own limit
     a.total_rows = min(rows) if rows else 1 << 20
@@ -355,6 +379,7 @@ def make_table_args(kv_len, verify_len, block_table, table_len, free_pages, free
 
 def fd_step_tables(args: fd_table_args, stream=None) -> None:
     """Pages of a step change hands, then its row offsets, page lists, positions and slots are written."""
+    _launchable(args.device)
     _check(load().fd_step_tables(C.byref(args), _stream(stream)))
 
 
@@ -362,31 +387,47 @@ def fd_qk_norm_rope(q, k, q_out, k_out, positions, inv_freq, *, q_weight=None, k
                     interleaved: bool = False, stream=None) -> None:
     """q [R, Hq, D], k (and v) [R, Hkv, D]: any strides between rows and heads; outputs dense.  rotary_dim is twice the number of
     inv_freq's entries (None: no rotation)."""
-    R, Hq, D = q.shape
-    Hkv, dt = k.shape[1], q.dtype
+    shape = q.shape
+    R, Hq, D = shape
+    kshape, dt, device = k.shape, q.dtype, q.get_device()
+    Hkv = kshape[1]
     qs, ks = q.stride(), k.stride()
     vs = (0, 0, 1) if v is None else v.stride()
-    if not (k.shape == k_out.shape == (R, Hkv, D) and q_out.shape == q.shape and k.dtype == dt and q_out.dtype == dt and k_out.dtype == dt):
+    if not (kshape == k_out.shape == (R, Hkv, D) and q_out.shape == shape and k.dtype is dt and q_out.dtype is dt and k_out.dtype is dt):
         raise TypeError(f"q, q_out must be [{R}, {Hq}, {D}] and k, k_out [{R}, {Hkv}, {D}], all of {dt}")
     if (qs[2] != 1 and R * Hq) or (ks[2] != 1 and R * Hkv) or (vs[2] != 1 and R * Hkv):
         raise TypeError("q, k and v need a contiguous last dimension")
     if not (q_out.is_contiguous() and k_out.is_contiguous()):
         raise TypeError("q_out and k_out must be contiguous")
-    if v is not None and not (v_out is not None and v.shape == v_out.shape == k.shape and v.dtype == v_out.dtype == dt and v_out.is_contiguous()):
-        raise TypeError(f"v and v_out must be [{R}, {Hkv}, {D}] of {dt}, v_out contiguous")
-    for name, t in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if t is not None and (t.numel() != D or t.dtype != dt or not t.is_contiguous()):
-            raise TypeError(f"{name} must be {D} contiguous elements of {dt}")
+    one = k.get_device() == q_out.get_device() == k_out.get_device() == device
+    if v is not None:
+        if not (v_out is not None and v.shape == v_out.shape == kshape and v.dtype is dt and v_out.dtype is dt and v_out.is_contiguous()):
+            raise TypeError(f"v and v_out must be [{R}, {Hkv}, {D}] of {dt}, v_out contiguous")
+        one = one and v.get_device() == v_out.get_device() == device
+    if q_weight is not None:
+        if q_weight.numel() != D or q_weight.dtype is not dt or not q_weight.is_contiguous():
+            raise TypeError(f"q_weight must be {D} contiguous elements of {dt}")
+        one = one and q_weight.get_device() == device
+    if k_weight is not None:
+        if k_weight.numel() != D or k_weight.dtype is not dt or not k_weight.is_contiguous():
+            raise TypeError(f"k_weight must be {D} contiguous elements of {dt}")
+        one = one and k_weight.get_device() == device
     half = 0
     if inv_freq is not None:
         half = inv_freq.numel()
-        if inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous():
+        if inv_freq.dtype is not torch.float32 or not inv_freq.is_contiguous():
             raise TypeError("inv_freq must be contiguous float32")
-        if half and (positions is None or positions.numel() != R):
-            raise TypeError(f"positions must have {R} entries")
+        one = one and inv_freq.get_device() == device
+        if half:
+            if positions is None or positions.numel() != R:
+                raise TypeError(f"positions must have {R} entries")
+            one = one and positions.get_device() == device
+    if not one:
+        raise TypeError("the tensors are on different devices")
+    _launchable(device)
     a = fd_rope_args(R, Hq, Hkv, D, 2 * half, 1 if interleaved else 0, _dtype_code(q), eps, q.data_ptr(), k.data_ptr(), _ptr(v), qs[0], qs[1], ks[0], ks[1],
                      vs[0], vs[1], q_out.data_ptr(), k_out.data_ptr(), _ptr(v_out), _ptr(q_weight), _ptr(k_weight), _ptr(inv_freq),
-                     _opt_i32(positions, "positions"))
+                     _i32(positions, "positions").data_ptr() if half else None)
     _check(load().fd_qk_norm_rope(C.byref(a), _stream(stream)))
 
 
@@ -411,6 +452,7 @@ class Q4Cache:
                 raise TypeError(f"{name}: pages and heads must lie as those of k_codes do, in blocks")
         self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
         self.num_pages, self.num_kv_heads, self.page_size, self.head_dim = P, H, ps, D
+        self.device = _one_device(k_codes, k_scales, v_codes, v_scales)
         self.c = fd_q4_cache(k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr(),
                              k_codes.stride(0) // max(1, ps * half), k_codes.stride(1) // max(1, ps * half))
 
@@ -429,9 +471,22 @@ def make_attn_args_q4(q, k_new, v_new, cache: Q4Cache, page_indptr, page_indices
     """make_attn_args for a cache in 4 bits: fd_verify_draft_attn_q4 and fd_append_kv_q4 take the cache beside the struct."""
     if cache.num_kv_heads != k_new.shape[1] or cache.head_dim != q.shape[2]:
         raise TypeError("the cache's heads or head dim are not those of the rows")
+    R, B = q.shape[0], kv_len.shape[0]
+    for name, t, shape in (("k_new", k_new, (R, cache.num_kv_heads, cache.head_dim)), ("v_new", v_new, k_new.shape), ("out", out, q.shape)):
+        if t.shape != shape or t.dtype != q.dtype:
+            raise TypeError(f"{name} must be {tuple(shape)} of {q.dtype}")
+    if lse is not None and not (lse.shape == q.shape[:2] and lse.dtype == torch.float32 and lse.is_contiguous()):
+        raise TypeError(f"lse must be {tuple(q.shape[:2])} of float32")
+    for name, t, n in (("page_indptr", page_indptr, B + 1), ("row_indptr", row_indptr, B + 1), ("verify_len", verify_len, B), ("mask_vis", mask_vis, B),
+                       ("mask_blocks", mask_blocks, B)):
+        if t is not None and t.numel() != n:
+            raise TypeError(f"{name} must have {n} entries")
     a = make_attn_args(q, k_new, v_new, cache.k_codes, cache.k_codes, page_indptr, page_indices, kv_len, row_indptr, verify_len, mask_vis,
                        mask_blocks, out=out, lse=lse, max_kv_len=max_kv_len, max_new_rows=max_new_rows, sm_scale=sm_scale, flags=flags,
                        kv_chunk=kv_chunk, workspace=workspace, status=status)
+    a.device = _one_device(cache.k_codes, q, k_new, v_new, page_indptr, page_indices, kv_len, row_indptr, verify_len, mask_vis, mask_blocks, out, lse,
+                           workspace, status)
+    a.cache = cache
     a.k_cache = a.v_cache = None
     a.cache_stride_page = a.cache_stride_head = a.cache_stride_token = 0
     return a
@@ -441,27 +496,52 @@ def fd_verify_draft_attn_q4_workspace(args: fd_attn_args) -> int:
     return int(load().fd_verify_draft_attn_q4_workspace(C.byref(args)))
 
 
+def _fits(args: fd_attn_args, cache: Q4Cache) -> None:
+    """The call was made for this cache, or for one like it."""
+    if cache is args.cache:
+        return _launchable(cache.device)
+    if (args.num_kv_heads, args.head_dim, args.page_size) != (cache.num_kv_heads, cache.head_dim, cache.page_size) or args.num_pages > cache.num_pages:
+        raise TypeError("the cache is not of the shape that the call was made for")
+    if args.device != cache.device:
+        raise TypeError("the cache is on another device than the call's tensors")
+    _launchable(cache.device)
+
+
 def fd_verify_draft_attn_q4(args: fd_attn_args, cache: Q4Cache, stream=None) -> None:
-    """Enqueue the attention call described by `args` over the 4-bit `cache`."""
+    """Enqueue the attention call described by `args` (make_attn_args_q4) over the 4-bit `cache`."""
+    _fits(args, cache)
     _check(load().fd_verify_draft_attn_q4(C.byref(args), C.byref(cache.c), _stream(stream)))
 
 
 def fd_append_kv_q4(args: fd_attn_args, cache: Q4Cache, accept_len, kv_len_out, stream=None) -> None:
-    """Round and commit new rows 0 .. accept_len[i] of the call described by `args` to the 4-bit `cache`."""
-    _check(load().fd_append_kv_q4(C.byref(args), C.byref(cache.c), _ptr(_i32(accept_len, "accept_len")),
-                                  _ptr(_i32(kv_len_out, "kv_len_out")), _stream(stream)))
+    """Round and commit new rows 0 .. accept_len[i] of the call described by `args` (make_attn_args_q4) to the 4-bit `cache`."""
+    _fits(args, cache)
+    B = args.batch
+    if accept_len.numel() != B or kv_len_out.numel() != B:
+        raise TypeError(f"accept_len and kv_len_out must have {B} entries")
+    if not accept_len.get_device() == kv_len_out.get_device() == args.device:
+        raise TypeError("accept_len and kv_len_out are on another device than the call's tensors")
+    _check(load().fd_append_kv_q4(C.byref(args), C.byref(cache.c), _i32(accept_len, "accept_len").data_ptr(),
+                                  _i32(kv_len_out, "kv_len_out").data_ptr(), _stream(stream)))
 
 
 def fd_read_kv_q4(cache: Q4Cache, page_indptr, page_indices, start, out_indptr, k_out, v_out, *, status=None, stream=None) -> None:
     """Tokens start[i] .. of every sequence as rows out_indptr[i] .. of k_out / v_out [R, Hkv, D], float32 or bfloat16."""
-    R = k_out.shape[0]
-    if not (k_out.shape == v_out.shape == (R, cache.num_kv_heads, cache.head_dim) and k_out.dtype == v_out.dtype and k_out.is_contiguous() and
+    shape, dt, device = k_out.shape, k_out.dtype, cache.device
+    if not (shape == v_out.shape and shape[1:] == (cache.num_kv_heads, cache.head_dim) and v_out.dtype is dt and k_out.is_contiguous() and
             v_out.is_contiguous()):
         raise TypeError(f"k_out and v_out must be contiguous, [rows, {cache.num_kv_heads}, {cache.head_dim}], both of one dtype")
+    B = out_indptr.numel() - 1
+    if B < 0 or page_indptr.numel() != B + 1 or (start is not None and start.numel() != B):
+        raise TypeError("out_indptr and page_indptr must have one entry more than there are sequences, start one each")
+    if not k_out.get_device() == v_out.get_device() == page_indptr.get_device() == page_indices.get_device() == out_indptr.get_device() == device or \
+            (start is not None and start.get_device() != device) or (status is not None and status.get_device() != device):
+        raise TypeError("the tensors are on different devices")
+    _launchable(device)
     _check(load().fd_read_kv_q4(
-        C.byref(cache.c), out_indptr.shape[0] - 1, cache.num_kv_heads, cache.head_dim, cache.page_size, cache.num_pages,
-        _ptr(_i32(page_indptr, "page_indptr")), _ptr(_i32(page_indices, "page_indices")), page_indices.numel(), _opt_i32(start, "start"),
-        _ptr(_i32(out_indptr, "out_indptr")), R, _ptr(k_out), _ptr(v_out), _dtype_code(k_out), _ptr(status), _stream(stream)))
+        C.byref(cache.c), B, cache.num_kv_heads, cache.head_dim, cache.page_size, cache.num_pages,
+        _i32(page_indptr, "page_indptr").data_ptr(), _i32(page_indices, "page_indices").data_ptr(), page_indices.numel(), _opt_i32(start, "start"),
+        _i32(out_indptr, "out_indptr").data_ptr(), shape[0], k_out.data_ptr(), v_out.data_ptr(), _dtype_code(k_out), _ptr(status), _stream(stream)))
 
 
 def fd_version() -> str:

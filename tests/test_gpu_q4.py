@@ -205,6 +205,16 @@ def test_larger_batch_without_a_chunk(fd):
     call.check(*call.run())
 
 
+@pytest.mark.parametrize("B,hkv", [(64, 8), (65, 2), (100, 1), (130, 4), (257, 1)])
+def test_batches(fd, B, hkv):
+    """Lengths of up to 64 sequences, of up to 256 and of more; pieces in one round and, the longest first, in several."""
+    rng = np.random.default_rng(B)
+    kv = np.where(rng.random(B) < 0.1, rng.integers(800, 1500, size=B), rng.integers(0, 200, size=B))
+    call = Q4Call(fd, kv=kv, k=rng.integers(0, 3, size=B), m=rng.integers(0, 2, size=B), hq=2 * hkv, hkv=hkv, seed=B).upload()
+    call.check(*call.run())
+    assert int(call.status.item()) == 0
+
+
 def test_scale_and_sharp_scores(fd):
     """Scores that spread over some hundred units of base 2: the running maximum moves often."""
     call = Q4Call(fd, kv=[400, 900], k=[4, 4], m=[4, 4], std=6.0, seed=8).upload(sm_scale=0.3)

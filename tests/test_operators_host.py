@@ -169,3 +169,49 @@ def test_binding_checks_shapes():
     with pytest.raises(TypeError, match="table_len"):
         i = lambda n: z(n, dt=torch.int32)  # noqa: E731
         fd.make_table_args(i(2), i(2), z(2, 4, dt=torch.int32), i(3), i(8), i(1), page_size=16, row_indptr=i(3), page_indptr=i(3), page_indices=i(8))
+
+
+def test_binding_refuses_tensors_that_no_kernel_may_touch():
+    """Tensors in host memory, sizes that contradict each other, a cache of another shape than the call was made for."""
+    z = lambda *s, dt=torch.bfloat16: torch.zeros(s, dtype=dt)  # noqa: E731
+    i = lambda n: z(n, dt=torch.int32)  # noqa: E731
+    q, k = z(3, 8, 128), z(3, 2, 128)
+    with pytest.raises(TypeError, match="CPU"):
+        fd.fd_qk_norm_rope(q, k, q, k, i(3), torch.ones(64))
+    tables = lambda **kw: fd.make_table_args(i(2), i(2), z(2, 4, dt=torch.int32), i(2), i(8), i(1), page_size=16, row_indptr=i(3), page_indptr=i(3),  # noqa: E731
+                                             page_indices=i(8), **kw)
+    with pytest.raises(TypeError, match="CPU"):
+        fd.fd_step_tables(tables())
+    c = fd.alloc_q4_cache(6, 2, 32, 128, device="cpu")
+    with pytest.raises(TypeError, match="CPU"):
+        fd.fd_read_kv_q4(c, i(3), i(6), None, i(3), z(5, 2, 128), z(5, 2, 128))
+    with pytest.raises(TypeError, match="one entry more"):
+        fd.fd_read_kv_q4(c, i(2), i(6), None, i(3), z(5, 2, 128), z(5, 2, 128))
+    with pytest.raises(TypeError, match="start"):
+        fd.fd_read_kv_q4(c, i(3), i(6), i(3), i(3), z(5, 2, 128), z(5, 2, 128))
+    good = dict(q=q, k_new=k, v_new=k, cache=c, page_indptr=i(3), page_indices=i(6), kv_len=i(2), row_indptr=i(3), verify_len=i(2), out=q, max_kv_len=9,
+                max_new_rows=3)
+    args = fd.make_attn_args_q4(**good)
+    assert args.device == -1 and args.num_pages == 6
+    for kw, words in ((dict(k_new=z(2, 2, 128)), "k_new"), (dict(v_new=z(3, 1, 128)), "v_new"), (dict(out=z(3, 8, 128, dt=torch.float32)), "out"),
+                      (dict(lse=z(3, 8)), "lse"), (dict(lse=z(3, 4, dt=torch.float32)), "lse"), (dict(row_indptr=i(2)), "row_indptr"),
+                      (dict(page_indptr=i(2)), "page_indptr"), (dict(verify_len=i(3)), "verify_len"), (dict(mask_vis=i(1)), "mask_vis"),
+                      (dict(k_new=z(3, 4, 128)), "heads")):
+        with pytest.raises(TypeError, match=words):
+            fd.make_attn_args_q4(**dict(good, **kw))
+    for other in (fd.alloc_q4_cache(5, 2, 32, 128, device="cpu"), fd.alloc_q4_cache(6, 2, 16, 128, device="cpu"), fd.alloc_q4_cache(6, 2, 32, 64, device="cpu"),
+                  fd.alloc_q4_cache(6, 4, 32, 128, device="cpu")):
+        for call in (lambda: fd.fd_verify_draft_attn_q4(args, other), lambda: fd.fd_append_kv_q4(args, other, i(2), i(2))):
+            with pytest.raises(TypeError, match="made for"):
+                call()
+    with pytest.raises(TypeError, match="CPU"):
+        fd.fd_verify_draft_attn_q4(args, c)
+    with pytest.raises(TypeError, match="CPU"):
+        fd.fd_append_kv_q4(args, c, i(2), i(2))
+
+
+def test_launches_that_are_too_large_are_refused():
+    need = lambda **kw: fd.load().fd_verify_draft_attn_q4_workspace(C.byref(_attn(**kw)))  # noqa: E731
+    assert need(batch=65535, num_kv_heads=8, total_rows=1 << 20, max_new_rows=32) > 0
+    assert need(batch=65535, num_kv_heads=32, total_rows=1 << 24, max_new_rows=2048) == 0
+    _refused(_rope(total_rows=(1 << 25) + 1), 2, "2^25")
