@@ -332,42 +332,6 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
     look_up(0, at0, at1);
     request_keys(ka, at0, at1);
     request_values(va, at0, at1);
-    look_up(1, at0, at1);
-    request_keys(kb, at0, at1);
-    request_values(vb, at0, at1);
-  }
-  // The query as the sum of two e4m3 numbers: q = 2^u hi + 2^(u-5) lo with 2^u hi up to 2^(u+8) the row's largest magnitude.  hi keeps four significant
-  // bits, what is left of a bf16's eight fits four more: exact for all but elements 2^-14 of the largest, and those to 2^-22 of it.
-  i32x8 qh[NA], ql[NA];
-  int uh, ul;                                            // exponents + 127, a byte
-  {
-    unsigned top = 0;
-#pragma unroll
-    for (int t = 0; t < 4 * NA; ++t)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) top = max(top, max(qw[t][e] & 0x7fff0000u, (qw[t][e] << 16) & 0x7fff0000u));
-    const auto both = __builtin_amdgcn_permlane32_swap(top, top, false, false);
-    top = max(both[0], both[1]);
-    const int b = clampi((int)(top >> 23) - 7, 6, 247);
-    uh = b; ul = top < 0x7f800000u ? b - 5 : 255;        // (a row with an infinity or a NaN: its scores are NaN)
-    const float up = __uint_as_float((unsigned)(254 - b) << 23);
-#pragma unroll
-    for (int a = 0; a < NA; ++a)
-#pragma unroll
-      for (int w = 0; w < 8; ++w) {                      // a word: four elements
-        const u32x4 x = qw[4 * a + w / 2];
-        const unsigned x0 = x[w % 2 * 2], x1 = x[w % 2 * 2 + 1];
-        const float f[4] = {__uint_as_float(x0 << 16) * up, __uint_as_float(x0 & 0xffff0000u) * up, __uint_as_float(x1 << 16) * up, __uint_as_float(x1 & 0xffff0000u) * up};
-        int hi = 0, lo = 0;
-        hi = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], hi, false);
-        hi = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], hi, true);
-        const f32x2 h0 = __builtin_amdgcn_cvt_pk_f32_fp8(hi, false), h1 = __builtin_amdgcn_cvt_pk_f32_fp8(hi, true);
-        lo = __builtin_amdgcn_cvt_pk_fp8_f32((f[0] - h0[0]) * 32.f, (f[1] - h0[1]) * 32.f, lo, false);
-        lo = __builtin_amdgcn_cvt_pk_fp8_f32((f[2] - h1[0]) * 32.f, (f[3] - h1[1]) * 32.f, lo, true);
-        qh[a][w] = row_on ? hi : 0;
-        ql[a][w] = row_on ? lo : 0;
-      }
-    if (!row_on) ul = 127;
   }
   const float scale2 = p.sm_scale * 1.44269504088896340736f;
 
@@ -405,6 +369,146 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
     }
     l += sum;
   };
+  // ---- the sequence's own rows, in bf16: keys as the first operand straight from memory, values through this wave's part of LDS and its transposing read ----
+  int b = first > cached ? first : cached;               // the wave's first block at or behind `cached`
+  b += (slot - (b - first)) & (KS - 1);
+  if (b < last) {
+    constexpr int VP = DH + 32;                          // pitch of a row of values, bf16: the four rows of a transposing read use every bank once
+    static_assert(32 * VP * sizeof(bf16_t) <= sizeof(lds_o[0]), "a block of values fits a wave's part of LDS");
+    constexpr int LPR = DH / 8, RPL = 64 / LPR;          // lanes of a row, rows of a load
+    bf16_t* lv = reinterpret_cast<bf16_t*>(&lds_o[wave][0][0]);
+    const RowWindow win = row_window(nr, s);
+    const long long stride = (long long)p.Hkv * DH;
+    const bf16_t* k0 = reinterpret_cast<const bf16_t*>(p.k_new) + s.row0 * stride + (long long)pc.head * DH;
+    const bf16_t* v0 = reinterpret_cast<const bf16_t*>(p.v_new) + s.row0 * stride + (long long)pc.head * DH;
+    u32x4 kf[STEPS], vr[STEPS];
+    // (behind the last row: that row, which the mask leaves out)
+    auto load_k = [&](int t0) FD_INLINE {
+      const bf16_t* krow = k0 + min(t0 + key_of_row, s.n - 1) * stride;
+#pragma unroll
+      for (int t = 0; t < STEPS; ++t) kf[t] = *reinterpret_cast<const u32x4*>(krow + 64 * (t / 4) + 32 * (t / 2 % 2) + 16 * h + 8 * (t % 2));
+    };
+    auto load_v = [&](int t0) FD_INLINE {
+#pragma unroll
+      for (int t = 0; t < STEPS; ++t) vr[t] = *reinterpret_cast<const u32x4*>(v0 + min(t0 + RPL * t + lane / LPR, s.n - 1) * stride + lane % LPR * 8);
+    };
+    load_k(32 * (b - cached));
+    load_v(32 * (b - cached));
+    for (; b < last; b += KS) {
+      const int t0 = 32 * (b - cached);
+      // A value that is no number must not reach a row that does not see it, and zero times it is NaN: it enters the product as zero.
+      unsigned odd = 0;                                  // (an exponent of all ones, plus one in its last place, reaches the sign)
+#pragma unroll
+      for (int t = 0; t < STEPS; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) odd |= (vr[t][e] & 0x7f807f80u) + 0x00800080u;
+      const bool any_odd = __any((odd & 0x80008000u) != 0);
+      if (any_odd) {
+#pragma unroll
+        for (int t = 0; t < STEPS; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if ((vr[t][e] & 0x7f80u) == 0x7f80u) vr[t][e] &= 0xffff0000u;
+            if ((vr[t][e] & 0x7f800000u) == 0x7f800000u) vr[t][e] &= 0xffffu;
+          }
+      }
+      __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+#pragma unroll
+      for (int t = 0; t < STEPS; ++t) *reinterpret_cast<u32x4*>(lv + (RPL * t + lane / LPR) * VP + lane % LPR * 8) = vr[t];
+      f32x16 x;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[e] = 0.f;
+#pragma unroll
+      for (int t = 0; t < STEPS; ++t) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kf[t]), as_bf16x8(qw[t]), x, 0, 0, 0);
+      if (b + KS < last) { load_k(t0 + 32 * KS); load_v(t0 + 32 * KS); }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int t = t0 + 16 * (e / 8) + 8 * h + e % 8;
+        x[e] = ((t < s.n) & new_key_visible(win, t)) ? x[e] : -INFINITY;
+      }
+      f32x16 y;
+      const float sum = exponentials(x, y);
+      settle(x, y, sum);
+      x = y;
+      __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+      // (sixteen lanes read four keys of sixteen channels, and each gets its channel's four)
+      const bf16_t* vt = lv + (8 * h + ((lane & 15) >> 2)) * VP + (l31 & 16) + 4 * (lane & 3);
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        u32x4 pf;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) pf[e] = pack_bf16x2(x[8 * q + 2 * e], x[8 * q + 2 * e + 1]);
+#pragma unroll
+        for (int cc = 0; cc < NC; ++cc) {
+          const s16x4 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + 16 * q * VP + 32 * cc));
+          const s16x4 w = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + (16 * q + 4) * VP + 32 * cc));
+          const s16x8 v = {u[0], u[1], u[2], u[3], w[0], w[1], w[2], w[3]};
+          o[cc] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), as_bf16x8(pf), o[cc], 0, 0, 0);
+        }
+      }
+      if (any_odd) {                                     // rare: infinities and NaN are added one by one where they are seen
+        float* mine = &lds_o[wave][l31][0];              // (a row's 32 probabilities, in place of the values)
+        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+#pragma unroll
+        for (int e = 0; e < 16; ++e) mine[16 * (e / 8) + 8 * h + e % 8] = x[e];
+        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+        const int n = min(32, s.n - t0);
+#pragma unroll 1
+        for (int t = 0; t < n; ++t) {
+          if (!new_key_visible(win, t0 + t)) continue;
+          const float pr = mine[t];
+          const bf16_t* vrow = v0 + (t0 + t) * stride + 4 * h;
+#pragma unroll
+          for (int cc = 0; cc < NC; ++cc)
+#pragma unroll
+            for (int a = 0; a < 16; ++a) {
+              const float v = bf16_to_f32(vrow[32 * cc + 8 * (a / 4) + a % 4]);
+              if (!(fabsf(v) < INFINITY)) o[cc][a] += pr * v;
+            }
+        }
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+  }
+  if (count > 0) {
+    unsigned at0, at1;
+    look_up(1, at0, at1);
+    request_keys(kb, at0, at1);
+    request_values(vb, at0, at1);
+  }
+  // The query as the sum of two e4m3 numbers: q = 2^u hi + 2^(u-5) lo with 2^u hi up to 2^(u+8) the row's largest magnitude.  hi keeps four significant
+  // bits, what is left of a bf16's eight fits four more: exact for all but elements 2^-14 of the largest, and those to 2^-22 of it.
+  i32x8 qh[NA], ql[NA];
+  int uh, ul;                                            // exponents + 127, a byte
+  {
+    unsigned top = 0;
+#pragma unroll
+    for (int t = 0; t < 4 * NA; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) top = max(top, max(qw[t][e] & 0x7fff0000u, (qw[t][e] << 16) & 0x7fff0000u));
+    const auto both = __builtin_amdgcn_permlane32_swap(top, top, false, false);
+    top = max(both[0], both[1]);
+    const int b = clampi((int)(top >> 23) - 7, 6, 247);
+    uh = b; ul = top < 0x7f800000u ? b - 5 : 255;        // (a row with an infinity or a NaN: its scores are NaN)
+    const float up = __uint_as_float((unsigned)(254 - b) << 23);
+#pragma unroll
+    for (int a = 0; a < NA; ++a)
+#pragma unroll
+      for (int w = 0; w < 8; ++w) {                      // a word: four elements
+        const u32x4 x = qw[4 * a + w / 2];
+        const unsigned x0 = x[w % 2 * 2], x1 = x[w % 2 * 2 + 1];
+        const float f[4] = {__uint_as_float(x0 << 16) * up, __uint_as_float(x0 & 0xffff0000u) * up, __uint_as_float(x1 << 16) * up, __uint_as_float(x1 & 0xffff0000u) * up};
+        int hi = 0, lo = 0;
+        hi = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], hi, false);
+        hi = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], hi, true);
+        const f32x2 h0 = __builtin_amdgcn_cvt_pk_f32_fp8(hi, false), h1 = __builtin_amdgcn_cvt_pk_f32_fp8(hi, true);
+        lo = __builtin_amdgcn_cvt_pk_fp8_f32((f[0] - h0[0]) * 32.f, (f[1] - h0[1]) * 32.f, lo, false);
+        lo = __builtin_amdgcn_cvt_pk_fp8_f32((f[2] - h1[0]) * 32.f, (f[3] - h1[1]) * 32.f, lo, true);
+        qh[a][w] = row_on ? hi : 0;
+        ql[a][w] = row_on ? lo : 0;
+      }
+    if (!row_on) ul = 127;
+  }
   auto key_scores = [&](const Q4Keys<DH>& r) FD_INLINE {
     f32x16 x;
 #pragma unroll
@@ -493,112 +597,6 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
     }
   }
 
-  // ---- the sequence's own rows, in bf16: keys as the first operand straight from memory, values through this wave's part of LDS and its transposing read ----
-  int b = first > cached ? first : cached;               // the wave's first block at or behind `cached`
-  b += (slot - (b - first)) & (KS - 1);
-  if (b < last) {
-    constexpr int VP = DH + 32;                          // pitch of a row of values, bf16: the four rows of a transposing read use every bank once
-    static_assert(32 * VP * sizeof(bf16_t) <= sizeof(lds_o[0]), "a block of values fits a wave's part of LDS");
-    constexpr int LPR = DH / 8, RPL = 64 / LPR;          // lanes of a row, rows of a load
-    bf16_t* lv = reinterpret_cast<bf16_t*>(&lds_o[wave][0][0]);
-    const RowWindow win = row_window(nr, s);
-    const long long stride = (long long)p.Hkv * DH;
-    const bf16_t* k0 = reinterpret_cast<const bf16_t*>(p.k_new) + s.row0 * stride + (long long)pc.head * DH;
-    const bf16_t* v0 = reinterpret_cast<const bf16_t*>(p.v_new) + s.row0 * stride + (long long)pc.head * DH;
-    u32x4 qf[STEPS], kf[STEPS], vr[STEPS];
-#pragma unroll
-    for (int t = 0; t < STEPS; ++t) qf[t] = *reinterpret_cast<const u32x4*>(qrow + 64 * (t / 4) + 32 * h + 8 * (t % 4));
-    // (behind the last row: that row, which the mask leaves out)
-    auto load_k = [&](int t0) FD_INLINE {
-      const bf16_t* krow = k0 + min(t0 + key_of_row, s.n - 1) * stride;
-#pragma unroll
-      for (int t = 0; t < STEPS; ++t) kf[t] = *reinterpret_cast<const u32x4*>(krow + 64 * (t / 4) + 32 * h + 8 * (t % 4));
-    };
-    auto load_v = [&](int t0) FD_INLINE {
-#pragma unroll
-      for (int t = 0; t < STEPS; ++t) vr[t] = *reinterpret_cast<const u32x4*>(v0 + min(t0 + RPL * t + lane / LPR, s.n - 1) * stride + lane % LPR * 8);
-    };
-    load_k(32 * (b - cached));
-    load_v(32 * (b - cached));
-#pragma unroll
-    for (int t = 0; t < STEPS; ++t)
-      if (!row_on) qf[t] = u32x4{0, 0, 0, 0};
-    for (; b < last; b += KS) {
-      const int t0 = 32 * (b - cached);
-      // A value that is no number must not reach a row that does not see it, and zero times it is NaN: it enters the product as zero.
-      unsigned odd = 0;                                  // (an exponent of all ones, plus one in its last place, reaches the sign)
-#pragma unroll
-      for (int t = 0; t < STEPS; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) odd |= (vr[t][e] & 0x7f807f80u) + 0x00800080u;
-      const bool any_odd = __any((odd & 0x80008000u) != 0);
-      if (any_odd) {
-#pragma unroll
-        for (int t = 0; t < STEPS; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if ((vr[t][e] & 0x7f80u) == 0x7f80u) vr[t][e] &= 0xffff0000u;
-            if ((vr[t][e] & 0x7f800000u) == 0x7f800000u) vr[t][e] &= 0xffffu;
-          }
-      }
-      __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-#pragma unroll
-      for (int t = 0; t < STEPS; ++t) *reinterpret_cast<u32x4*>(lv + (RPL * t + lane / LPR) * VP + lane % LPR * 8) = vr[t];
-      f32x16 x;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) x[e] = 0.f;
-#pragma unroll
-      for (int t = 0; t < STEPS; ++t) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kf[t]), as_bf16x8(qf[t]), x, 0, 0, 0);
-      if (b + KS < last) { load_k(t0 + 32 * KS); load_v(t0 + 32 * KS); }
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int t = t0 + 16 * (e / 8) + 8 * h + e % 8;
-        x[e] = ((t < s.n) & new_key_visible(win, t)) ? x[e] : -INFINITY;
-      }
-      f32x16 y;
-      const float sum = exponentials(x, y);
-      settle(x, y, sum);
-      x = y;
-      __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-      // (sixteen lanes read four keys of sixteen channels, and each gets its channel's four)
-      const bf16_t* vt = lv + (8 * h + ((lane & 15) >> 2)) * VP + (l31 & 16) + 4 * (lane & 3);
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        u32x4 pf;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) pf[e] = pack_bf16x2(x[8 * q + 2 * e], x[8 * q + 2 * e + 1]);
-#pragma unroll
-        for (int cc = 0; cc < NC; ++cc) {
-          const s16x4 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + 16 * q * VP + 32 * cc));
-          const s16x4 w = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + (16 * q + 4) * VP + 32 * cc));
-          const s16x8 v = {u[0], u[1], u[2], u[3], w[0], w[1], w[2], w[3]};
-          o[cc] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), as_bf16x8(pf), o[cc], 0, 0, 0);
-        }
-      }
-      if (any_odd) {                                     // rare: infinities and NaN are added one by one where they are seen
-        float* mine = &lds_o[wave][l31][0];              // (a row's 32 probabilities, in place of the values)
-        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-#pragma unroll
-        for (int e = 0; e < 16; ++e) mine[16 * (e / 8) + 8 * h + e % 8] = x[e];
-        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-        const int n = min(32, s.n - t0);
-#pragma unroll 1
-        for (int t = 0; t < n; ++t) {
-          if (!new_key_visible(win, t0 + t)) continue;
-          const float pr = mine[t];
-          const bf16_t* vrow = v0 + (t0 + t) * stride + 4 * h;
-#pragma unroll
-          for (int cc = 0; cc < NC; ++cc)
-#pragma unroll
-            for (int a = 0; a < 16; ++a) {
-              const float v = bf16_to_f32(vrow[32 * cc + 8 * (a / 4) + a % 4]);
-              if (!(fabsf(v) < INFINITY)) o[cc][a] += pr * v;
-            }
-        }
-      }
-    }
-    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-  }
   l = add_halves(l);
 
   // ---- the waves' parts of a row meet: O^T columns become rows of LDS ----
