@@ -27,6 +27,9 @@ constexpr float Q4_LAZY = 256.f;          // sum of a row's sixteen probabilitie
 constexpr int Q4_SLOTS = 512;             // work-groups that run at once: two a compute unit
 constexpr int Q4_PIECES = 512;            // pieces aimed at where there are more than Q4_SLOTS / 2 items
 constexpr int Q4_CLASSES = 4;             // lengths of pieces that are told apart
+// A block of own rows takes as long as Q4_OWN of cached ones, the first Q4_OWN_START more (2 sequences of 272 new rows 66.2 us a call, 1 of 16 new
+// rows 16.5; counted as cached ones 74.8 and 17.7).
+constexpr int Q4_OWN = 3, Q4_OWN_START = 4;
 constexpr int Q4_MIN_PIECE = 8;           // blocks of a piece, at least (but for the last of a short item)
 constexpr int Q4_KEPT = 4;                // rounds of 64 sequences whose lengths a wave keeps in LDS
 
@@ -46,8 +49,8 @@ __device__ __forceinline__ int q4_row_blocks(int rows) { return rows <= 32 ? 1 :
 // How long a block takes a work-group, in halves: four waves take four blocks of one row block side by side, or one block of four.
 __device__ __forceinline__ int q4_weight(int rows) { return rows <= 32 ? 2 : rows <= 64 ? 3 : 6; }
 
-// Blocks of a sequence's keys, and its tile rows: rows / 128 whole items and one of what is left.
-__device__ __forceinline__ int q4_blocks(const SeqInfo& s) { return s.n > 0 ? (s.L + Q4_TK - 1) / Q4_TK + (s.n + Q4_TK - 1) / Q4_TK : 0; }
+// Length of a sequence's keys in blocks, own ones counted Q4_OWN times, and its tile rows: rows / 128 whole items and one of what is left.
+__device__ __forceinline__ int q4_blocks(const SeqInfo& s) { return s.n > 0 ? (s.L + Q4_TK - 1) / Q4_TK + Q4_OWN_START + Q4_OWN * ((s.n + Q4_TK - 1) / Q4_TK) : 0; }
 __device__ __forceinline__ long long q4_units(int blocks, int rows) {           // of one head: weight x blocks
   const int tail = rows % Q4_ROWS;
   return (long long)blocks * (rows / Q4_ROWS * q4_weight(Q4_ROWS) + (tail ? q4_weight(tail) : 0));
@@ -256,8 +259,12 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
   const int rows = min(Q4_ROWS, s.n * p.G - pc.rt * Q4_ROWS);
   const int RB = q4_row_blocks(rows), ks_shift = RB == 1 ? 2 : RB == 2 ? 1 : 0, KS = 1 << ks_shift;
   const int rb = wave & (RB - 1), slot = wave >> (2 - ks_shift);
-  const int cached = (s.L + Q4_TK - 1) / Q4_TK, blocks = cached + (s.n + Q4_TK - 1) / Q4_TK;
-  const int first = (int)((long long)blocks * pc.piece / pc.pieces), last = (int)((long long)blocks * (pc.piece + 1) / pc.pieces);
+  const int cached = (s.L + Q4_TK - 1) / Q4_TK, length = q4_blocks(s);
+  auto cut = [&](int piece) FD_INLINE {                  // blocks before a piece
+    const int at = (int)((long long)length * piece / pc.pieces);
+    return at <= cached ? at : cached + max(at - cached - Q4_OWN_START, 0) / Q4_OWN;
+  };
+  const int first = cut(pc.piece), last = cut(pc.piece + 1);
 
   // ---- cached keys: which blocks, where they lie ----
   const int lo = first + slot, hi = min(last, cached);
@@ -733,7 +740,7 @@ static Q4Shape q4_shape(int batch, int num_kv_heads, int group, int total_rows, 
   z.fixed = kv_chunk / Q4_TK;
   const long long seqs = batch < total_rows ? batch : total_rows;       // sequences that have rows
   z.items = seqs * num_kv_heads * z.rt_max;
-  const long long blocks = ((long long)max_kv_len + Q4_TK - 1) / Q4_TK + (max_new_rows + Q4_TK - 1) / Q4_TK;
+  const long long blocks = ((long long)max_kv_len + Q4_TK - 1) / Q4_TK + Q4_OWN_START + Q4_OWN * ((max_new_rows + Q4_TK - 1) / Q4_TK);
   // units of all sequences' work: sequences whose rows add up to total_rows at most, every one as long as may be
   const double units = ((double)total_rows * group / 32 + 2.0 * seqs) * 2 * (double)blocks;
   z.unit_shift = 0;
