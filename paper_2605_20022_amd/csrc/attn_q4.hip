@@ -27,8 +27,8 @@ constexpr float Q4_LAZY = 256.f;          // sum of a row's sixteen probabilitie
 constexpr int Q4_SLOTS = 512;             // work-groups that run at once: two a compute unit
 constexpr int Q4_PIECES = 512;            // pieces aimed at where there are more than Q4_SLOTS / 2 items
 constexpr int Q4_CLASSES = 4;             // lengths of pieces that are told apart
-// A block of own rows takes as long as Q4_OWN of cached ones, the first Q4_OWN_START more (2 sequences of 272 new rows 66.2 us a call, 1 of 16 new
-// rows 16.5; counted as cached ones 74.8 and 17.7).
+// A block of own rows takes as long as Q4_OWN of cached ones, the first Q4_OWN_START more (1 sequence of 16 new rows 16.4 us a call; counted as a
+// cached one 17.7, with 6 more 17.2.  2 of 272, in 17 blocks: 62.2, with 6 more 63.7).
 constexpr int Q4_OWN = 3, Q4_OWN_START = 4;
 constexpr int Q4_MIN_PIECE = 8;           // blocks of a piece, at least (but for the last of a short item)
 constexpr int Q4_KEPT = 4;                // rounds of 64 sequences whose lengths a wave keeps in LDS
@@ -49,8 +49,14 @@ __device__ __forceinline__ int q4_row_blocks(int rows) { return rows <= 32 ? 1 :
 // How long a block takes a work-group, in halves: four waves take four blocks of one row block side by side, or one block of four.
 __device__ __forceinline__ int q4_weight(int rows) { return rows <= 32 ? 2 : rows <= 64 ? 3 : 6; }
 
-// Length of a sequence's keys in blocks, own ones counted Q4_OWN times, and its tile rows: rows / 128 whole items and one of what is left.
-__device__ __forceinline__ int q4_blocks(const SeqInfo& s) { return s.n > 0 ? (s.L + Q4_TK - 1) / Q4_TK + Q4_OWN_START + Q4_OWN * ((s.n + Q4_TK - 1) / Q4_TK) : 0; }
+// How long a sequence's keys take, in cached blocks: the own rows' blocks that one of its rows sees (its own mask block's keys lie in two of them or
+// so) count Q4_OWN each, the first Q4_OWN_START more.
+__device__ __forceinline__ int q4_own(const SeqInfo& s) {
+  const int all = (s.n + Q4_TK - 1) / Q4_TK;
+  return Q4_OWN * (s.nb > 1 ? min((s.k + Q4_TK - 1) / Q4_TK + 2, all) : all);
+}
+__device__ __forceinline__ int q4_blocks(const SeqInfo& s) { return s.n > 0 ? (s.L + Q4_TK - 1) / Q4_TK + Q4_OWN_START + q4_own(s) : 0; }
+// An item's tile rows: rows / 128 whole items and one of what is left.
 __device__ __forceinline__ long long q4_units(int blocks, int rows) {           // of one head: weight x blocks
   const int tail = rows % Q4_ROWS;
   return (long long)blocks * (rows / Q4_ROWS * q4_weight(Q4_ROWS) + (tail ? q4_weight(tail) : 0));
@@ -259,10 +265,11 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
   const int rows = min(Q4_ROWS, s.n * p.G - pc.rt * Q4_ROWS);
   const int RB = q4_row_blocks(rows), ks_shift = RB == 1 ? 2 : RB == 2 ? 1 : 0, KS = 1 << ks_shift;
   const int rb = wave & (RB - 1), slot = wave >> (2 - ks_shift);
-  const int cached = (s.L + Q4_TK - 1) / Q4_TK, length = q4_blocks(s);
+  const int cached = (s.L + Q4_TK - 1) / Q4_TK, own = (s.n + Q4_TK - 1) / Q4_TK, length = q4_blocks(s);
+  const float own_at = (float)own / (float)q4_own(s);
   auto cut = [&](int piece) FD_INLINE {                  // blocks before a piece
-    const int at = (int)((long long)length * piece / pc.pieces);
-    return at <= cached ? at : cached + max(at - cached - Q4_OWN_START, 0) / Q4_OWN;
+    const int at = (int)((long long)length * piece / pc.pieces), in_own = max(at - cached - Q4_OWN_START, 0);
+    return at <= cached ? at : at == length ? cached + own : cached + min((int)((float)in_own * own_at), own);
   };
   const int first = cut(pc.piece), last = cut(pc.piece + 1);
 
@@ -379,12 +386,23 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
   // ---- the sequence's own rows, in bf16: keys as the first operand straight from memory, values through this wave's part of LDS and its transposing read ----
   int b = first > cached ? first : cached;               // the wave's first block at or behind `cached`
   b += (slot - (b - first)) & (KS - 1);
+  RowWindow win = row_window(nr, s);
+  if (!row_on) win = RowWindow{0, 0, 0};
+  // a block that none of the wave's rows sees is passed over (2 sequences of 16 verify rows and 16 mask blocks of 16, where a row sees one: 66.2 -> 62.2 us)
+  auto seen_from = [&](int b) FD_INLINE {
+    while (b < last) {
+      const int t0 = 32 * (b - cached);
+      if (__any((t0 < win.vr) | ((t0 < win.hi) & (t0 + 32 > win.lo)))) break;
+      b += KS;
+    }
+    return b;
+  };
+  b = seen_from(b);
   if (b < last) {
     constexpr int VP = DH + 32;                          // pitch of a row of values, bf16: the four rows of a transposing read use every bank once
     static_assert(32 * VP * sizeof(bf16_t) <= sizeof(lds_o[0]), "a block of values fits a wave's part of LDS");
     constexpr int LPR = DH / 8, RPL = 64 / LPR;          // lanes of a row, rows of a load
     bf16_t* lv = reinterpret_cast<bf16_t*>(&lds_o[wave][0][0]);
-    const RowWindow win = row_window(nr, s);
     const long long stride = (long long)p.Hkv * DH;
     const bf16_t* k0 = reinterpret_cast<const bf16_t*>(p.k_new) + s.row0 * stride + (long long)pc.head * DH;
     const bf16_t* v0 = reinterpret_cast<const bf16_t*>(p.v_new) + s.row0 * stride + (long long)pc.head * DH;
@@ -401,7 +419,8 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
     };
     load_k(32 * (b - cached));
     load_v(32 * (b - cached));
-    for (; b < last; b += KS) {
+    for (int next; b < last; b = next) {
+      next = seen_from(b + KS);
       const int t0 = 32 * (b - cached);
       // A value that is no number must not reach a row that does not see it, and zero times it is NaN: it enters the product as zero.
       unsigned odd = 0;                                  // (an exponent of all ones, plus one in its last place, reaches the sign)
@@ -427,7 +446,7 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
       for (int e = 0; e < 16; ++e) x[e] = 0.f;
 #pragma unroll
       for (int t = 0; t < STEPS; ++t) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kf[t]), as_bf16x8(qw[t]), x, 0, 0, 0);
-      if (b + KS < last) { load_k(t0 + 32 * KS); load_v(t0 + 32 * KS); }
+      if (next < last) { load_k(32 * (next - cached)); load_v(32 * (next - cached)); }
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const int t = t0 + 16 * (e / 8) + 8 * h + e % 8;
