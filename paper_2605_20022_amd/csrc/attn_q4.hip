@@ -76,7 +76,7 @@ __device__ __forceinline__ Q4Count q4_count(const Q4Sched& sc, int blocks, int r
 // How long a sequence's longest piece takes a work-group, in units.
 __device__ __forceinline__ int q4_longest(const Q4Sched& sc, int blocks, int rows, float density) {
   const int r = min(rows, Q4_ROWS);
-  return rows > 0 ? (int)((float)blocks * (float)q4_weight(r) / (float)q4_pieces(sc, blocks, r, density)) : 0;
+  return rows > 0 ? (int)((float)blocks * (float)q4_weight(r) * __builtin_amdgcn_rcpf((float)q4_pieces(sc, blocks, r, density))) : 0;
 }
 
 struct Q4Piece { int head, rt, piece, pieces, slot, item; SeqInfo s; };
@@ -106,10 +106,10 @@ __device__ __forceinline__ bool q4_find(const AttnParams& p, const Q4Sched& sc, 
   const int rounds = FEW ? 1 : (p.B + 63) / 64;
   SeqInfo only = {};
   auto load = [&](int c) FD_INLINE {
-    SeqInfo s = {};
     uint32_t bad = 0;
     const int i = c * 64 + lane;
-    if (i < p.B) s = load_seq_t<false>(p, i, &bad);
+    SeqInfo s = load_seq_t<false>(p, min(i, p.B - 1), &bad);       // (no branch: the loads of two rounds go together)
+    if (i >= p.B) s.n = 0;
     if (bad && w == 0 && threadIdx.x < 64) flag_status(p.status, bad);        // (work-group 0 comes by every sequence)
     return s;
   };
@@ -120,9 +120,7 @@ __device__ __forceinline__ bool q4_find(const AttnParams& p, const Q4Sched& sc, 
     return SeqInfo{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
   };
   int total = 0, items = 0;                              // units of one head, in 2^unit_shift (the host's bounds say that they fit), and items
-#pragma unroll 1
-  for (int c = 0; c < rounds; ++c) {
-    const SeqInfo s = load(c);
+  auto count = [&](int c, const SeqInfo& s) FD_INLINE {
     if (FEW) only = s;
     else if (c < Q4_KEPT) {
       kept[(c * 2) * 64 + lane] = make_int4(s.L, s.row0, s.n, s.k);
@@ -132,7 +130,15 @@ __device__ __forceinline__ bool q4_find(const AttnParams& p, const Q4Sched& sc, 
     // (rounded up, so that there are never more pieces than the host counts on)
     total += wave_total((int)((q4_units(q4_blocks(s), rows) + (1ll << sc.unit_shift) - 1) >> sc.unit_shift));
     items += wave_total((rows + Q4_ROWS - 1) / Q4_ROWS);
-  }
+  };
+  if (FEW) count(0, load(0));
+  else
+#pragma unroll 1
+    for (int c = 0; c < rounds; c += 2) {
+      const SeqInfo s0 = load(c), s1 = load(c + 1);      // (behind the last sequence: without rows)
+      count(c, s0);
+      count(c + 1, s1);
+    }
   const float all = ldexpf((float)total, sc.unit_shift) * (float)p.Hkv * 1.000001f;
   float density = (float)Q4_PIECES / fmaxf(all, 1.f);
   int classes = 1;
