@@ -1,18 +1,24 @@
 // Hybrid-mask verify+draft attention (Sec. 4.1) over a KV cache held in 4 bits, head dim 128 or 64.
 //
 // An item is one (sequence, KV head, up to 128 tile rows); a tile row is (new row, query head of the group).  Its keys,
-// cached ones and then the sequence's own new rows, form blocks of 32.  Items are cut into pieces of equal length, one per
+// cached ones and then the sequence's own new rows, form blocks of 32.  Items are cut into pieces of about equal time, one per
 // work-group; an item of several pieces leaves (maximum, sum, un-normalised O) partials for the combine kernel.
 //
 // A wave takes 32 tile rows and a stream of blocks, by itself: with up to 32 tile rows the four waves of a work-group
 // take every fourth block, with up to 64 two waves a row block take every second, else each wave has its own rows and all blocks.
-// They meet once, when the piece ends and their (maximum, sum, O) are merged through LDS.  Nothing of the cache goes through LDS:
-//   S^T = K Q^T    v_mfma_f32_32x32x16_bf16.  A lane's eight channels of a key are one word of codes, so a lane loads its
-//                  half of a key's codes (sixteen bytes each 64 channels, one scale) and converts them in registers
-//   O^T += V^T P^T the layout of v_codes holds eight keys of a channel in one word for the same reason; the scale of a
-//                  value (one a token and head) is multiplied into P, which a lane holds for eight keys in a row
+// They meet once, when the piece ends and their (maximum, sum, O) are merged through LDS.  Nothing of the cache goes through LDS, and two blocks of a
+// wave are on their way while a third is worked on:
+//   S^T = K Q^T    v_mfma_scale_f32_32x32x64_f8f6f4: codes and scales of the keys as they lie in memory (a lane's sixteen bytes are its
+//                  half of a key's 64 channels), the query as the sum of two e4m3 numbers, which holds what bf16 holds.  Two products of 33 ns
+//                  each 64 channels, where codes converted to bf16 would take four of 15 and 32 conversions of 2
+//   O^T += V^T P^T v_mfma_f32_32x32x16_bf16.  The layout of v_codes holds eight keys of a channel in one word, which four instructions make bf16,
+//                  exactly; the scale of a value (one a token and head) is multiplied into P, which a lane holds for eight keys in a row
 // Which key a row of S^T stands for is free: row i = (b4 b3 b2 b1 b0) is key (b4 b2 b3 b1 b0), so that the sixteen scores that a lane holds
 // are two runs of eight keys, as the second product wants them.
+//
+// What bounds it: a block of 32 rows and 32 keys takes a SIMD 0.25 us of matrix instructions and 0.24 us of others, of which little runs side by side
+// (0.47 us measured, two waves): 2 sequences of 2048 to 8192 keys, 272 rows and 32 query heads 62.0 us a call, 734 TFLOP/s.  With few rows HBM: 128
+// sequences of 1024 to 8192 keys, up to 16 rows 171 us, 3.9 TB/s.  One short sequence is latency (16.2 us): lengths, pages, codes, merge, second launch.
 #include "kv_q4.h"
 #include <type_traits>
 
@@ -144,7 +150,7 @@ __device__ __forceinline__ bool q4_find(const AttnParams& p, const Q4Sched& sc, 
   int classes = 1;
   float part = 0.f;                                      // classes a unit of time
   if (sc.fixed <= 0 && rounds <= Q4_KEPT) {
-    if (items * (long long)p.Hkv <= Q4_SLOTS / 2) {
+    if (items * (long long)p.Hkv < Q4_SLOTS) {
       // first whether pieces of Q4_MIN_PIECE blocks fit, then between what fits and what is too many
       float lo = (float)(Q4_SLOTS - items * p.Hkv) / fmaxf(all, 1.f), hi = (float)Q4_SLOTS / fmaxf(all, 1.f);
       density = 1.f;
@@ -777,7 +783,7 @@ static Q4Shape q4_shape(int batch, int num_kv_heads, int group, int total_rows, 
     // pieces - 1 of an item are density x units at most, which sum to Q4_PIECES over all items (Q4_SLOTS in one round)
     static_assert(Q4_SLOTS <= Q4_PIECES, "what one round takes is within the bounds of several");
     // (work-groups without a piece are not free, 0.8 us for 528 of them: none where one round is sure to do)
-    const bool one_round = z.items <= Q4_SLOTS / 2 && batch <= 64 * Q4_KEPT;
+    const bool one_round = z.items < Q4_SLOTS && batch <= 64 * Q4_KEPT;
     z.wgs = one_round ? Q4_SLOTS : z.items + Q4_PIECES;
     z.partials = one_round ? Q4_SLOTS : 2 * Q4_PIECES;                  // an item in c >= 2 pieces: c <= 2 (c - 1)
     const long long most = z.items * (blocks / Q4_MIN_PIECE + 1);
