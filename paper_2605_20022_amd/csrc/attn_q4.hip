@@ -703,11 +703,13 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
 }
 
 // Merge of the partials of split items, by rows: a row is taken by TPR = DH / 8 lanes, eight channels each.  AT_ONCE pieces at a time, lane j of them
-// knows the maximum and sum of piece j; their values are requested with those, so that a batch is one latency.
+// knows the maximum and sum of piece j; their values are requested with those, so that a batch is one latency.  Where an item may have many pieces,
+// 2^group_shift such groups of lanes share a row's and meet in LDS (1 sequence of 16 384 keys, 64 pieces an item: MEASURED).
 template <int DH>
-__global__ __launch_bounds__(256) void attn_q4_combine_kernel(AttnParams p, Q4Sched sc) {
+__global__ __launch_bounds__(256) void attn_q4_combine_kernel(AttnParams p, Q4Sched sc, int group_shift) {
   typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
-  constexpr int TPR = DH / 8, RPB = 256 / TPR, AT_ONCE = 8;
+  constexpr int TPR = DH / 8, SETS = 256 / TPR, AT_ONCE = 8;
+  __shared__ float lds_acc[SETS][DH + 4], lds_ml[SETS][2];
   const int item = blockIdx.x, rt = item % sc.rt_max, head = item / sc.rt_max % p.Hkv, seq = item / sc.rt_max / p.Hkv;
   const int2 e = sc.entries[item];
   // (a sequence without new rows, or with fewer, has no such item: what stands in its entry is old)
@@ -715,14 +717,17 @@ __global__ __launch_bounds__(256) void attn_q4_combine_kernel(AttnParams p, Q4Sc
   const int row0 = clampi(r0, 0, p.total_rows), new_rows = min(clampi(r1 - r0, 0, p.max_new_rows), p.total_rows - row0);
   const int rows = min(Q4_ROWS, new_rows * p.G - rt * Q4_ROWS);
   const int pieces = __builtin_amdgcn_readfirstlane(e.x), slot = __builtin_amdgcn_readfirstlane(e.y);
-  const int r = blockIdx.y * RPB + threadIdx.x / TPR, part = threadIdx.x % TPR;
-  if ((int)blockIdx.y * RPB >= rows || pieces <= 1 || slot < 0 || (long long)slot + pieces > sc.max_partials) return;
+  const int rows_here = SETS >> group_shift, first_row = (int)blockIdx.y * rows_here;
+  if (first_row >= rows || pieces <= 1 || slot < 0 || (long long)slot + pieces > sc.max_partials) return;
+  const int set = threadIdx.x / TPR, group = set >> (31 - __clz(SETS) - group_shift);         // (sets of one row are rows_here apart)
+  const int r = first_row + (set & (rows_here - 1)), part = threadIdx.x % TPR;
   const int rr = r < rows ? r : 0;                       // (every lane takes part in the exchanges)
   const int j = part % AT_ONCE, lane0 = (threadIdx.x & 63) / TPR * TPR;
   float M = -3e38f, sum = 0.f, acc[8] = {};
-  for (int q0 = 0; q0 < pieces; q0 += AT_ONCE) {
-    const int n = min(AT_ONCE, pieces - q0);
-    const long long at = (long long)(slot + q0) * Q4_ROWS + rr;
+  for (int q0 = 0; q0 < pieces; q0 += AT_ONCE << group_shift) {
+    const int q = q0 + group * AT_ONCE, n = min(AT_ONCE, pieces - q);
+    if (n <= 0) break;                                   // (the same for all lanes of a set)
+    const long long at = (long long)(slot + q) * Q4_ROWS + rr;
     f32x4 ml = {-3e38f, 0.f, 0.f, 0.f};
     if (j < n) ml = *reinterpret_cast<const f32x4*>(sc.part_ml + (at + (long long)j * Q4_ROWS) * 4);
     u32x4 w[AT_ONCE];
@@ -743,12 +748,34 @@ __global__ __launch_bounds__(256) void attn_q4_combine_kernel(AttnParams p, Q4Sc
     for (int u = 0; u < 8; ++u) acc[u] *= shrink;
 #pragma unroll
     for (int u = 0; u < AT_ONCE; ++u) {
-      if (u >= n) break;                                 // (uniform; no zero times an infinity)
+      if (u >= n) break;                                 // (no zero times an infinity)
       const float g = __shfl(weight, lane0 + u);
       const f16x8 v = __builtin_bit_cast(f16x8, w[u]);
 #pragma unroll
       for (int k = 0; k < 8; ++k) acc[k] += g * (float)v[k];
     }
+  }
+  if (group_shift > 0) {
+    if (part == 0) { lds_ml[set][0] = M; lds_ml[set][1] = sum; }
+#pragma unroll
+    for (int k = 0; k < 8; k += 4) *reinterpret_cast<f32x4*>(&lds_acc[set][part * 8 + k]) = f32x4{acc[k], acc[k + 1], acc[k + 2], acc[k + 3]};
+    __syncthreads();
+    if (group > 0) return;
+    const int groups = min(1 << group_shift, (pieces + AT_ONCE - 1) / AT_ONCE);      // those that had a piece
+    float top = M;
+    for (int k = 1; k < groups; ++k) top = fmaxf(top, lds_ml[set + k * rows_here][0]);
+    const float f0 = __builtin_amdgcn_exp2f(M - top);
+    sum *= f0;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) acc[u] *= f0;
+    for (int k = 1; k < groups; ++k) {
+      const int o = set + k * rows_here;
+      const float f = __builtin_amdgcn_exp2f(lds_ml[o][0] - top);
+      sum += f * lds_ml[o][1];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) acc[u] += f * lds_acc[o][part * 8 + u];
+    }
+    M = top;
   }
   if (r >= rows) return;
   const int t = rt * Q4_ROWS + r, n = t / p.G;
@@ -762,7 +789,7 @@ __global__ __launch_bounds__(256) void attn_q4_combine_kernel(AttnParams p, Q4Sc
 }
 
 // Items of the largest sequence, partial slots and work-groups that there can be, and the workspace.
-struct Q4Shape { long long items, partials, wgs; int rt_max, fixed, unit_shift; size_t off_ml, off_entries, total; };
+struct Q4Shape { long long items, partials, wgs, max_pieces; int rt_max, fixed, unit_shift; size_t off_ml, off_entries, total; };
 static Q4Shape q4_shape(int batch, int num_kv_heads, int group, int total_rows, int max_kv_len, int max_new_rows, int kv_chunk, int head_dim) {
   Q4Shape z;
   const long long tile_rows = (long long)max_new_rows * group;
@@ -776,8 +803,9 @@ static Q4Shape q4_shape(int batch, int num_kv_heads, int group, int total_rows, 
   const double units = ((double)total_rows * group / 32 + 2.0 * seqs) * 2 * (double)blocks;
   z.unit_shift = 0;
   while (units / (double)(1ll << z.unit_shift) >= 1073741824.0) ++z.unit_shift;
+  z.max_pieces = blocks / (z.fixed > 0 ? z.fixed : Q4_MIN_PIECE) + 1;
   if (z.fixed > 0) {
-    z.wgs = z.items * (blocks / z.fixed + 1);
+    z.wgs = z.items * z.max_pieces;
     z.partials = z.wgs;
   } else {
     // pieces - 1 of an item are density x units at most, which sum to Q4_PIECES over all items (Q4_SLOTS in one round)
@@ -786,7 +814,7 @@ static Q4Shape q4_shape(int batch, int num_kv_heads, int group, int total_rows, 
     const bool one_round = z.items < Q4_SLOTS && batch <= 64 * Q4_KEPT;
     z.wgs = one_round ? Q4_SLOTS : z.items + Q4_PIECES;
     z.partials = one_round ? Q4_SLOTS : 2 * Q4_PIECES;                  // an item in c >= 2 pieces: c <= 2 (c - 1)
-    const long long most = z.items * (blocks / Q4_MIN_PIECE + 1);
+    const long long most = z.items * z.max_pieces;
     if (most < z.wgs) z.wgs = most;
     if (most < z.partials) z.partials = most;
   }
@@ -809,16 +837,20 @@ hipError_t run_attn_q4(const AttnParams& p, const Q4Cache& c, void* workspace, i
   char* ws = reinterpret_cast<char*>(workspace);
   const Q4Sched sc = {z.fixed, z.fixed > 0 ? 1.f / (float)z.fixed : 0.f, z.unit_shift, z.rt_max, (int)z.partials, reinterpret_cast<unsigned short*>(ws), reinterpret_cast<float*>(ws + z.off_ml), reinterpret_cast<int2*>(ws + z.off_entries)};
   if (z.wgs == 0) return hipSuccess;
-  const int per_row = p.D / 8, most_rows = (int)((long long)p.max_new_rows * p.G < Q4_ROWS ? p.max_new_rows * p.G : Q4_ROWS);
-  const dim3 grid((unsigned)((long long)p.B * p.Hkv * z.rt_max), (most_rows * per_row + 255) / 256);
+  // Pieces of an item, if the call's items are about equal: eight of them to a group of lanes.
+  const int sets = 256 / (p.D / 8), most_rows = (int)((long long)p.max_new_rows * p.G < Q4_ROWS ? p.max_new_rows * p.G : Q4_ROWS);
+  const long long pieces = z.fixed > 0 ? z.max_pieces : z.max_pieces < Q4_SLOTS / z.items ? z.max_pieces : Q4_SLOTS / z.items;
+  int group_shift = 0;
+  while ((8ll << group_shift) < pieces && (2 << group_shift) <= sets) ++group_shift;
+  const dim3 grid((unsigned)((long long)p.B * p.Hkv * z.rt_max), (most_rows + (sets >> group_shift) - 1) / (sets >> group_shift));
   if (p.D == 128) {
     if (p.B <= 64) hipLaunchKernelGGL((attn_q4_kernel<128, true>), dim3((unsigned)z.wgs), dim3(Q4_BLOCK), 0, st, p, c, sc);
     else hipLaunchKernelGGL((attn_q4_kernel<128, false>), dim3((unsigned)z.wgs), dim3(Q4_BLOCK), 0, st, p, c, sc);
-    hipLaunchKernelGGL(attn_q4_combine_kernel<128>, grid, dim3(256), 0, st, p, sc);
+    hipLaunchKernelGGL(attn_q4_combine_kernel<128>, grid, dim3(256), 0, st, p, sc, group_shift);
   } else {
     if (p.B <= 64) hipLaunchKernelGGL((attn_q4_kernel<64, true>), dim3((unsigned)z.wgs), dim3(Q4_BLOCK), 0, st, p, c, sc);
     else hipLaunchKernelGGL((attn_q4_kernel<64, false>), dim3((unsigned)z.wgs), dim3(Q4_BLOCK), 0, st, p, c, sc);
-    hipLaunchKernelGGL(attn_q4_combine_kernel<64>, grid, dim3(256), 0, st, p, sc);
+    hipLaunchKernelGGL(attn_q4_combine_kernel<64>, grid, dim3(256), 0, st, p, sc, group_shift);
   }
   return hipGetLastError();
 }
