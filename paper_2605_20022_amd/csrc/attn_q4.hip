@@ -704,7 +704,7 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
 
 // Merge of the partials of split items, by rows: a row is taken by TPR = DH / 8 lanes, eight channels each.  AT_ONCE pieces at a time, lane j of them
 // knows the maximum and sum of piece j; their values are requested with those, so that a batch is one latency.  Where an item may have many pieces,
-// 2^group_shift such groups of lanes share a row's and meet in LDS (1 sequence of 16 384 keys, 64 pieces an item: MEASURED).
+// 2^group_shift such groups of lanes share a row's and meet in LDS (1 sequence of 32 768 keys, 64 pieces an item: 27 us a call, without 47).
 template <int DH>
 __global__ __launch_bounds__(256) void attn_q4_combine_kernel(AttnParams p, Q4Sched sc, int group_shift) {
   typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
@@ -837,11 +837,12 @@ hipError_t run_attn_q4(const AttnParams& p, const Q4Cache& c, void* workspace, i
   char* ws = reinterpret_cast<char*>(workspace);
   const Q4Sched sc = {z.fixed, z.fixed > 0 ? 1.f / (float)z.fixed : 0.f, z.unit_shift, z.rt_max, (int)z.partials, reinterpret_cast<unsigned short*>(ws), reinterpret_cast<float*>(ws + z.off_ml), reinterpret_cast<int2*>(ws + z.off_entries)};
   if (z.wgs == 0) return hipSuccess;
-  // Pieces of an item, if the call's items are about equal: eight of them to a group of lanes.
+  // Pieces of an item, if the call's items are about equal: four of them to a group of lanes, so that twice as many are one batch (64 items of 4096 to
+  // 8192 keys 31.0 us a call, with eight 31.7, with two 31.0; 144 items of 272 rows 61.6, 61.7, 63.6).
   const int sets = 256 / (p.D / 8), most_rows = (int)((long long)p.max_new_rows * p.G < Q4_ROWS ? p.max_new_rows * p.G : Q4_ROWS);
   const long long pieces = z.fixed > 0 ? z.max_pieces : z.max_pieces < Q4_SLOTS / z.items ? z.max_pieces : Q4_SLOTS / z.items;
   int group_shift = 0;
-  while ((8ll << group_shift) < pieces && (2 << group_shift) <= sets) ++group_shift;
+  while ((4ll << group_shift) < pieces && (2 << group_shift) <= sets) ++group_shift;
   const dim3 grid((unsigned)((long long)p.B * p.Hkv * z.rt_max), (most_rows + (sets >> group_shift) - 1) / (sets >> group_shift));
   if (p.D == 128) {
     if (p.B <= 64) hipLaunchKernelGGL((attn_q4_kernel<128, true>), dim3((unsigned)z.wgs), dim3(Q4_BLOCK), 0, st, p, c, sc);
