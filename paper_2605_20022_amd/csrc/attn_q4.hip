@@ -31,12 +31,15 @@ constexpr int Q4_TK = 32;                 // keys of a block
 constexpr int Q4_ROWS = 128;              // tile rows of an item
 constexpr float Q4_LAZY = 256.f;          // sum of a row's sixteen probabilities from which on the softmax reference follows the row maximum
 constexpr int Q4_SLOTS = 512;             // work-groups that run at once: two a compute unit
-constexpr int Q4_PIECES = 512;            // pieces aimed at where there are more than Q4_SLOTS / 2 items
+// Units a compute unit up to which it takes one piece (one sequence of 32 768 keys, 64 rows, 99 units: 24.4 us a call, in twice as many pieces 27.4;
+// 4 of 8192 to 16 384, 146: 30.1 and 31.7; one of 131 072, 388: 52.8 and 52.0; 2 of 272 rows, 526: 88.9 and 61.7).
+constexpr int Q4_ALONE = 192;
+constexpr int Q4_PIECES = 512;            // pieces aimed at where there are Q4_SLOTS items or more
 constexpr int Q4_CLASSES = 4;             // lengths of pieces that are told apart
 // A block of own rows takes as long as Q4_OWN of cached ones, the first Q4_OWN_START more (1 sequence of 16 new rows 16.4 us a call; counted as a
 // cached one 17.7, with 6 more 17.2.  2 of 272, in 17 blocks: 62.2, with 6 more 63.7).
 constexpr int Q4_OWN = 3, Q4_OWN_START = 4;
-constexpr int Q4_MIN_PIECE = 8;           // blocks of a piece, at least (but for the last of a short item)
+constexpr int Q4_MIN_PIECE = 8;           // blocks of a piece, at least, but for the last of a short item (1 sequence of 1024 keys 14.9 us; 6: 15.7, 12: 15.5)
 constexpr int Q4_KEPT = 4;                // rounds of 64 sequences whose lengths a wave keeps in LDS
 
 struct Q4Sched {
@@ -100,7 +103,8 @@ __device__ __forceinline__ int wave_max(int v) {         // of values >= 0
 // Which piece work-group w takes: pieces are numbered by (class, sequence, head, item, piece).  Every wave finds it by itself, a sequence a lane, 64 at
 // a time: the lengths are one latency of memory, the rest LDS of its own and lane shifts, and no wave waits for another.  false: none.
 //
-// How many pieces: with at most Q4_SLOTS / 2 items as many as run at once, found by bisection, so that one round does it: a piece's start and
+// How many pieces: with fewer than Q4_SLOTS items as many as run at once, found by bisection, so that one round does it (128 items of 512 to 4096 keys
+// 27.8 us a call, in rounds 33.6; 384 of them 54, 59): a piece's start and
 // end cost about as much as twelve blocks (find, pages, first codes, merge), and a second round would wait for the first.  Else Q4_PIECES and
 // the items themselves, dealt out as work-groups become free, the sequences with the longest pieces first: one that began last would be waited for
 // (128 sequences of 1024 to 8192 keys: 170 us, in the order of the batch 200; 512 pieces and items 170, 640 176, 768 177).
@@ -151,8 +155,10 @@ __device__ __forceinline__ bool q4_find(const AttnParams& p, const Q4Sched& sc, 
   float part = 0.f;                                      // classes a unit of time
   if (sc.fixed <= 0 && rounds <= Q4_KEPT) {
     if (items * (long long)p.Hkv < Q4_SLOTS) {
-      // first whether pieces of Q4_MIN_PIECE blocks fit, then between what fits and what is too many
-      float lo = (float)(Q4_SLOTS - items * p.Hkv) / fmaxf(all, 1.f), hi = (float)Q4_SLOTS / fmaxf(all, 1.f);
+      // One a compute unit where that is not much work: two at a time start and end slower.  Then, first whether pieces of Q4_MIN_PIECE blocks fit,
+      // after that between what fits and what is too many.
+      const int slots = items * (long long)p.Hkv <= Q4_SLOTS / 4 && all <= (float)(Q4_SLOTS / 2 * Q4_ALONE) ? Q4_SLOTS / 2 : Q4_SLOTS;
+      float lo = (float)(slots - items * p.Hkv) / fmaxf(all, 1.f), hi = (float)slots / fmaxf(all, 1.f);
       density = 1.f;
 #pragma unroll 1
       for (int i = 0; i < 5; ++i) {
@@ -164,7 +170,7 @@ __device__ __forceinline__ bool q4_find(const AttnParams& p, const Q4Sched& sc, 
           const Q4Count k = q4_count(sc, q4_blocks(s), rows, density);
           n += rows / Q4_ROWS * k.full + k.tail;
         }
-        const bool fits = wave_total(n) * p.Hkv <= Q4_SLOTS;
+        const bool fits = wave_total(n) * p.Hkv <= slots;
         if (i == 0) { if (fits) { lo = density; break; } }
         else if (fits) lo = density;
         else hi = density;
