@@ -8,17 +8,19 @@
 // take every fourth block, with up to 64 two waves a row block take every second, else each wave has its own rows and all blocks.
 // They meet once, when the piece ends and their (maximum, sum, O) are merged through LDS.  Nothing of the cache goes through LDS, and two blocks of a
 // wave are on their way while a third is worked on:
-//   S^T = K Q^T    v_mfma_scale_f32_32x32x64_f8f6f4: codes and scales of the keys as they lie in memory (a lane's sixteen bytes are its
-//                  half of a key's 64 channels), the query as the sum of two e4m3 numbers, which holds what bf16 holds.  Two products of 33 ns
-//                  each 64 channels, where codes converted to bf16 would take four of 15 and 32 conversions of 2
-//   O^T += V^T P^T v_mfma_f32_32x32x16_bf16.  The layout of v_codes holds eight keys of a channel in one word, which four instructions make bf16,
-//                  exactly; the scale of a value (one a token and head) is multiplied into P, which a lane holds for eight keys in a row
+//   S^T = K Q^T    v_mfma_f32_32x32x16_bf16, with the query as it is: a lane's eight channels of a key are one word of codes, which four instructions
+//                  make bf16 times the key's power of two, exactly.  (The scaled instructions for 4 and 8 bits take the codes as they lie, with the
+//                  query as two e4m3 numbers, and 7% less time; but they add eight products at a time with some 14 bits below the largest: an lse of few
+//                  keys was 4e-5 off, and one large channel of a query drowned the others.)
+//   O^T += V^T P^T the same instruction.  The layout of v_codes holds eight keys of a channel in one word for the same reason;
+//                  the scale of a value (one a token and head) is multiplied into P, which a lane holds for eight keys in a row
 // Which key a row of S^T stands for is free: row i = (b4 b3 b2 b1 b0) is key (b4 b2 b3 b1 b0), so that the sixteen scores that a lane holds
 // are two runs of eight keys, as the second product wants them.
 //
-// What bounds it: a block of 32 rows and 32 keys takes a SIMD 0.25 us of matrix instructions and 0.24 us of others, of which little runs side by side
-// (0.47 us measured, two waves): 2 sequences of 2048 to 8192 keys, 272 rows and 32 query heads 62.0 us a call, 734 TFLOP/s.  With few rows HBM: 128
-// sequences of 1024 to 8192 keys, up to 16 rows 171 us, 3.9 TB/s.  One short sequence is latency (16.2 us): lengths, pages, codes, merge, second launch.
+// What bounds it: a block of 32 rows and 32 keys takes a SIMD 0.24 us of matrix instructions and 0.30 us of others, of which little runs side by side
+// (0.5 us measured, two waves): 2 sequences of 2048 to 8192 keys, 272 rows and 32 query heads 66.6 us a call, 684 TFLOP/s.  With few rows HBM, for which
+// the same arithmetic leaves little time: 128 sequences of 1024 to 8192 keys, up to 16 rows 181 us, 3.7 TB/s.  One short sequence is latency
+// (15.3 us): lengths, pages, codes, merge, second launch.
 #include "kv_q4.h"
 #include <type_traits>
 
@@ -248,16 +250,6 @@ __device__ __forceinline__ float add_halves(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-typedef __attribute__((ext_vector_type(8))) int i32x8;
-// x += K q^T over 64 channels: 32 codes of a key with their scale (byte BYTE of ks) and one part of the query with its exponent.
-template <int BYTE>
-__device__ __forceinline__ f32x16 scores(u32x4 k, unsigned ks, i32x8 q, int u, f32x16 x) {
-  typedef __attribute__((ext_vector_type(4))) int i32x4;
-  const i32x4 k4 = __builtin_bit_cast(i32x4, k);
-  const i32x8 a = __builtin_shufflevector(k4, k4, 0, 1, 2, 3, -1, -1, -1, -1);
-  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, q, x, 4, 0, BYTE, (int)ks, 0, u);       // formats: 4 = e2m1, 0 = e4m3
-}
-
 // Codes and scales of a block as a lane holds them.
 template <int DH> struct Q4Keys {
   u32x4 code[DH / 64];       // its key's channels 64 a + 32 h ..: 32 each
@@ -356,9 +348,9 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
   const int ti = pc.rt * Q4_ROWS + (row_on ? tr : 0);
   const int nr = ti / p.G, g = ti - nr * p.G;            // new row, query head of the group
   const bf16_t* qrow = reinterpret_cast<const bf16_t*>(p.q) + ((long long)(s.row0 + nr) * p.Hq + pc.head * p.G + g) * DH;
-  u32x4 qw[4 * NA];                                      // channels 64 a + 16 h .. and 64 a + 32 + 16 h .., sixteen each
+  u32x4 qw[4 * NA];                                      // channels 64 a + 32 h + 8 w ..: eight each, as the codes of a key lie
 #pragma unroll
-  for (int t = 0; t < 4 * NA; ++t) qw[t] = *reinterpret_cast<const u32x4*>(qrow + 64 * (t / 4) + 32 * (t / 2 % 2) + 16 * h + 8 * (t % 2));
+  for (int t = 0; t < 4 * NA; ++t) qw[t] = *reinterpret_cast<const u32x4*>(qrow + 64 * (t / 4) + 32 * h + 8 * (t % 4));
   if (count > 0) {
     unsigned at0, at1;
     look_up(0, at0, at1);
@@ -429,7 +421,7 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
     auto load_k = [&](int t0) FD_INLINE {
       const bf16_t* krow = k0 + min(t0 + key_of_row, s.n - 1) * stride;
 #pragma unroll
-      for (int t = 0; t < STEPS; ++t) kf[t] = *reinterpret_cast<const u32x4*>(krow + 64 * (t / 4) + 32 * (t / 2 % 2) + 16 * h + 8 * (t % 2));
+      for (int t = 0; t < STEPS; ++t) kf[t] = *reinterpret_cast<const u32x4*>(krow + 64 * (t / 4) + 32 * h + 8 * (t % 4));
     };
     auto load_v = [&](int t0) FD_INLINE {
 #pragma unroll
@@ -520,50 +512,17 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
     request_keys(kb, at0, at1);
     request_values(vb, at0, at1);
   }
-  // The query as the sum of two e4m3 numbers: q = 2^u hi + 2^(u-5) lo with 2^u hi up to 2^(u+8) the row's largest magnitude.  hi keeps four significant
-  // bits, what is left of a bf16's eight fits four more: exact for all but elements 2^-14 of the largest, and those to 2^-22 of it.
-  i32x8 qh[NA], ql[NA];
-  int uh, ul;                                            // exponents + 127, a byte
-  {
-    unsigned top = 0;
-#pragma unroll
-    for (int t = 0; t < 4 * NA; ++t)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) top = max(top, max(qw[t][e] & 0x7fff0000u, (qw[t][e] << 16) & 0x7fff0000u));
-    const auto both = __builtin_amdgcn_permlane32_swap(top, top, false, false);
-    top = max(both[0], both[1]);
-    const int b = clampi((int)(top >> 23) - 7, 6, 247);
-    uh = b; ul = top < 0x7f800000u ? b - 5 : 255;        // (a row with an infinity or a NaN: its scores are NaN)
-    const float up = __uint_as_float((unsigned)(254 - b) << 23);
-#pragma unroll
-    for (int a = 0; a < NA; ++a)
-#pragma unroll
-      for (int w = 0; w < 8; ++w) {                      // a word: four elements
-        const u32x4 x = qw[4 * a + w / 2];
-        const unsigned x0 = x[w % 2 * 2], x1 = x[w % 2 * 2 + 1];
-        const float f[4] = {__uint_as_float(x0 << 16) * up, __uint_as_float(x0 & 0xffff0000u) * up, __uint_as_float(x1 << 16) * up, __uint_as_float(x1 & 0xffff0000u) * up};
-        int hi = 0, lo = 0;
-        hi = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], hi, false);
-        hi = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], hi, true);
-        const f32x2 h0 = __builtin_amdgcn_cvt_pk_f32_fp8(hi, false), h1 = __builtin_amdgcn_cvt_pk_f32_fp8(hi, true);
-        lo = __builtin_amdgcn_cvt_pk_fp8_f32((f[0] - h0[0]) * 32.f, (f[1] - h0[1]) * 32.f, lo, false);
-        lo = __builtin_amdgcn_cvt_pk_fp8_f32((f[2] - h1[0]) * 32.f, (f[3] - h1[1]) * 32.f, lo, true);
-        qh[a][w] = row_on ? hi : 0;
-        ql[a][w] = row_on ? lo : 0;
-      }
-    if (!row_on) ul = 127;
-  }
+  // Eight codes of this lane's key with their power of two, as an operand: exact.
+  auto key_part = [&](const Q4Keys<DH>& r, int i) FD_INLINE {
+    const unsigned byte = (r.scale >> (8 * h) >> (16 * (i / 4))) & 255u;
+    return q4_to_bf16(r.code[i / 4][i % 4], q4_key_scale(byte));
+  };
   auto key_scores = [&](const Q4Keys<DH>& r) FD_INLINE {
     f32x16 x;
 #pragma unroll
     for (int e = 0; e < 16; ++e) x[e] = 0.f;
-    const unsigned ks = r.scale >> (8 * h);
-    x = scores<0>(r.code[0], ks, ql[0], ul, x);
-    x = scores<0>(r.code[0], ks, qh[0], uh, x);
-    if (NA == 2) {
-      x = scores<2>(r.code[NA - 1], ks, ql[NA - 1], ul, x);
-      x = scores<2>(r.code[NA - 1], ks, qh[NA - 1], uh, x);
-    }
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(key_part(r, i)), as_bf16x8(qw[i]), x, 0, 0, 0);
     return x;
   };
   // One block: its scores x become probabilities and weigh its values, while the matrix pipe works on the scores of the next.  left: keys of the
@@ -581,26 +540,28 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
         r.scale[e / 4][e % 4] = key >= left ? 0u : key + 1 >= left ? w & 0xffffu : w;
       }
     }
-    // a product for the next scores, then a share of the exponentials, in this order
+    // a product for the next scores, then the codes of the one after it and a share of the exponentials, in this order
     f32x16 y, xn;
-    float part[2 * NA];
-    const unsigned ks = next.scale >> (8 * h);
+    u32x4 kf[2];
+    float part[STEPS];
+    kf[0] = key_part(next, 0);
 #pragma unroll
     for (int e = 0; e < 16; ++e) xn[e] = 0.f;
 #pragma unroll
-    for (int i = 0; i < 2 * NA; ++i) {
-      constexpr int SHARE = 16 / (2 * NA);
+    for (int i = 0; i < STEPS; ++i) {
+      constexpr int SHARE = 16 / STEPS;
       __builtin_amdgcn_sched_barrier(0);
-      xn = i % 2 == 0 ? (i < 2 ? scores<0>(next.code[0], ks, ql[0], ul, xn) : scores<2>(next.code[NA - 1], ks, ql[NA - 1], ul, xn))
-                      : (i < 2 ? scores<0>(next.code[0], ks, qh[0], uh, xn) : scores<2>(next.code[NA - 1], ks, qh[NA - 1], uh, xn));
+      xn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kf[i & 1]), as_bf16x8(qw[i]), xn, 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
+      if (i + 1 < STEPS) kf[(i + 1) & 1] = key_part(next, i + 1);
       part[i] = 0.f;
 #pragma unroll
       for (int e = i * SHARE; e < (i + 1) * SHARE; ++e) y[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], scale2, -m));
 #pragma unroll
       for (int e = i * SHARE; e < (i + 1) * SHARE; e += 2) part[i] = e == i * SHARE ? y[e] + y[e + 1] : part[i] + (y[e] + y[e + 1]);
     }
-    const float sum = NA == 2 ? (part[0] + part[1]) + (part[2 * NA - 2] + part[2 * NA - 1]) : part[0] + part[1];
+    float sum = (part[0] + part[1]) + (part[2] + part[3]);
+    if (STEPS == 8) sum += (part[STEPS - 4] + part[STEPS - 3]) + (part[STEPS - 2] + part[STEPS - 1]);
     asm volatile("" : "+v"(xn));                         // (not to be moved past the branch)
     settle(x, y, sum);
     u32x4 pf[2];                                         // P times the values' scales

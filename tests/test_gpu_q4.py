@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import attention as oa
 from oracle import kv4
 from tests.q4_harness import Q4Call, assert_cache_is, bf16, bits_of, device_cache, i32
 
@@ -219,6 +220,33 @@ def test_scale_and_sharp_scores(fd):
     """Scores that spread over some hundred units of base 2: the running maximum moves often."""
     call = Q4Call(fd, kv=[400, 900], k=[4, 4], m=[4, 4], std=6.0, seed=8).upload(sm_scale=0.3)
     call.check(*call.run(), sm_scale=0.3)
+
+
+@pytest.mark.parametrize("dim", [128, 64])
+def test_one_large_channel(fd, dim):
+    """A channel of the query is a thousand times the others, and the scale keeps the softmax from being sharp: the small products count all the same."""
+    call = Q4Call(fd, kv=[3, 40, 700, 0], k=[2, 1, 4, 1], m=[0, 3, 4, 0], hq=8, hkv=2, dim=dim, seed=21)
+    q = oa.widen_bf16(call.q)
+    q[..., 5] *= 1024.0
+    call.q = bits_of(q)
+    call.upload(sm_scale=2.0 ** -9)
+    call.check(*call.run(), sm_scale=2.0 ** -9)
+
+
+@pytest.mark.parametrize("dim", [128, 64])
+def test_lse_of_few_keys(fd, dim):
+    """With a handful of keys nothing averages out.  A score is a sum of dim products in fp32, off by at most dim 2^-24 of the sum of their magnitudes, and
+    an lse by no more than its worst score; its maximum, exponentials, sum and logarithm add 2^-20 of max(1, |lse|)."""
+    call = Q4Call(fd, kv=[1, 2, 3, 5, 4], k=[1, 2, 4, 3, 1], m=[0] * 5, hq=16, hkv=4, dim=dim, seed=22).upload()
+    out, lse = call.run()
+    call.check(out, lse)
+    _, ref = call.oracle()
+    kmax = max(np.abs(call.cache.key_values()).max(), np.abs(oa.widen_bf16(call.k_new)).max())
+    q = np.abs(oa.widen_bf16(call.q))
+    bound = dim * 2.0 ** -24 * q.sum(-1) * kmax / np.sqrt(dim) + 2.0 ** -20 * np.maximum(1, np.abs(ref))
+    assert (np.abs(lse - ref) <= bound).all(), float((np.abs(lse - ref) / bound).max())
+    # and by far less where errors do not add up: half a step of fp32 a product, independent
+    assert np.sqrt(np.mean((lse - ref) ** 2)) <= 2.0 ** -20 * np.sqrt(np.mean(ref ** 2) + 1)
 
 
 def test_what_lies_behind_the_prefix_does_not_count(fd):
