@@ -10,7 +10,7 @@
 // wave are on their way while a third is worked on:
 //   S^T = K Q^T    v_mfma_f32_32x32x16_bf16, with the query as it is: a lane's eight channels of a key are one word of codes, which four instructions
 //                  make bf16 times the key's power of two, exactly.  (The scaled instructions for 4 and 8 bits take the codes as they lie, with the
-//                  query as two e4m3 numbers, and 7% less time; but they add eight products at a time with some 14 bits below the largest: an lse of few
+//                  query as two e4m3 numbers, and 3% less time; but they add eight products at a time with some 14 bits below the largest: an lse of few
 //                  keys was 4e-5 off, and one large channel of a query drowned the others.)
 //   O^T += V^T P^T the same instruction.  The layout of v_codes holds eight keys of a channel in one word for the same reason;
 //                  the scale of a value (one a token and head) is multiplied into P, which a lane holds for eight keys in a row
@@ -18,11 +18,10 @@
 // are two runs of eight keys, as the second product wants them.
 //
 // What bounds it: a block of 32 rows and 32 keys takes a SIMD 0.24 us of matrix instructions and 0.30 us of others, of which little runs side by side
-// (0.5 us measured, two waves): 2 sequences of 2048 to 8192 keys, 272 rows and 32 query heads 66.6 us a call, 684 TFLOP/s.  With few rows HBM, for which
-// the same arithmetic leaves little time: 128 sequences of 1024 to 8192 keys, up to 16 rows 181 us, 3.7 TB/s.  One short sequence is latency
-// (15.3 us): lengths, pages, codes, merge, second launch.
+// (0.5 us measured, two waves): 2 sequences of 2048 to 8192 keys, 272 rows and 32 query heads 64.0 us a call, 711 TFLOP/s.  With few rows HBM, for which
+// the same arithmetic leaves little time: 128 sequences of 1024 to 8192 keys, up to 16 rows 173 us, 3.9 TB/s.  One short sequence is latency
+// (15.2 us): lengths, pages, codes, merge, second launch.
 #include "kv_q4.h"
-#include <type_traits>
 
 namespace fd {
 
@@ -540,20 +539,16 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
         r.scale[e / 4][e % 4] = key >= left ? 0u : key + 1 >= left ? w & 0xffffu : w;
       }
     }
-    // a product for the next scores, then the codes of the one after it and a share of the exponentials, in this order
+    // products for the next scores, with a share of the exponentials in between; the compiler's order (held to this one by barriers for the
+    // scheduler, codes one product ahead: 4% slower)
     f32x16 y, xn;
-    u32x4 kf[2];
     float part[STEPS];
-    kf[0] = key_part(next, 0);
 #pragma unroll
     for (int e = 0; e < 16; ++e) xn[e] = 0.f;
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) {
       constexpr int SHARE = 16 / STEPS;
-      __builtin_amdgcn_sched_barrier(0);
-      xn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kf[i & 1]), as_bf16x8(qw[i]), xn, 0, 0, 0);
-      __builtin_amdgcn_sched_barrier(0);
-      if (i + 1 < STEPS) kf[(i + 1) & 1] = key_part(next, i + 1);
+      xn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(key_part(next, i)), as_bf16x8(qw[i]), xn, 0, 0, 0);
       part[i] = 0.f;
 #pragma unroll
       for (int e = i * SHARE; e < (i + 1) * SHARE; ++e) y[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], scale2, -m));
@@ -570,16 +565,9 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         pf[q][e] = pack_bf16x2(y[8 * q + 2 * e] * __uint_as_float(r.scale[q][e] << 16), y[8 * q + 2 * e + 1] * __uint_as_float(r.scale[q][e] & 0xffff0000u));
-    // codes are converted one product ahead, so that the matrix pipe does not wait for them
-    u32x4 vf[2];
-    vf[0] = q4_to_bf16(r.code[0][0], 1.f);
-    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int i = 0; i < 2 * NC; ++i) {
-      if (i + 1 < 2 * NC) vf[(i + 1) & 1] = q4_to_bf16(r.code[(i + 1) / NC][(i + 1) % NC], 1.f);
-      o[i % NC] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vf[i & 1]), as_bf16x8(pf[i / NC]), o[i % NC], 0, 0, 0);
-      __builtin_amdgcn_sched_barrier(0);
-    }
+    for (int i = 0; i < 2 * NC; ++i)
+      o[i % NC] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(q4_to_bf16(r.code[i / NC][i % NC], 1.f)), as_bf16x8(pf[i / NC]), o[i % NC], 0, 0, 0);
     return xn;
   };
   // Keys and values of two blocks are held or on their way.  Past the end the last block is requested again (its lines are at hand), so that
