@@ -33,14 +33,14 @@ constexpr int Q4_ROWS = 128;              // tile rows of an item
 constexpr float Q4_LAZY = 256.f;          // sum of a row's sixteen probabilities from which on the softmax reference follows the row maximum
 constexpr int Q4_SLOTS = 512;             // work-groups that run at once: two a compute unit
 // Units a compute unit up to which it takes one piece (one sequence of 32 768 keys, 64 rows, 99 units: 24.4 us a call, in twice as many pieces 27.4;
-// 4 of 8192 to 16 384, 146: 30.1 and 31.7; one of 131 072, 388: 52.8 and 52.0; 2 of 272 rows, 526: 88.9 and 61.7).
+// 4 of 8192 to 16 384, 146: 30.4 and 32.1; one of 8192, 272 rows, 420: 56.8 and 54.5).
 constexpr int Q4_ALONE = 192;
 constexpr int Q4_PIECES = 512;            // pieces aimed at where there are Q4_SLOTS items or more
 constexpr int Q4_CLASSES = 4;             // lengths of pieces that are told apart
-// A block of own rows takes as long as Q4_OWN of cached ones, the first Q4_OWN_START more (1 sequence of 16 new rows 16.4 us a call; counted as a
-// cached one 17.7, with 6 more 17.2.  2 of 272, in 17 blocks: 62.2, with 6 more 63.7).
+// A block of own rows takes as long as Q4_OWN of cached ones, the first Q4_OWN_START more (1 sequence of 16 new rows 15.1 us a call, 2 of 272 in 17
+// blocks 64.5; counted as cached ones 16.6 and 66.4, with 6 more 15.2 and 66.0).
 constexpr int Q4_OWN = 3, Q4_OWN_START = 4;
-constexpr int Q4_MIN_PIECE = 8;           // blocks of a piece, at least, but for the last of a short item (1 sequence of 1024 keys 14.9 us; 6: 15.7, 12: 15.5)
+constexpr int Q4_MIN_PIECE = 8;           // blocks of a piece, at least, but for the last of a short item (1 sequence of 1024 keys 14.1 us; 6: 14.8, 12: 14.6)
 constexpr int Q4_KEPT = 4;                // rounds of 64 sequences whose lengths a wave keeps in LDS
 
 struct Q4Sched {
@@ -104,13 +104,13 @@ __device__ __forceinline__ int wave_max(int v) {         // of values >= 0
 // Which piece work-group w takes: pieces are numbered by (class, sequence, head, item, piece).  Every wave finds it by itself, a sequence a lane, 64 at
 // a time: the lengths are one latency of memory, the rest LDS of its own and lane shifts, and no wave waits for another.  false: none.
 //
-// How many pieces: with fewer than Q4_SLOTS items as many as run at once, found by bisection, so that one round does it (128 items of 512 to 4096 keys
-// 27.8 us a call, in rounds 33.6; 384 of them 54, 59): a piece's start and
+// How many pieces: with fewer than Q4_SLOTS items as many as run at once, found by bisection, so that one round does it (16 sequences of 512 to
+// 4096 keys 26.6 us a call, in rounds 32.9; 2 of 272 rows 64.6, 78.9): a piece's start and
 // end cost about as much as twelve blocks (find, pages, first codes, merge), and a second round would wait for the first.  Else Q4_PIECES and
 // the items themselves, dealt out as work-groups become free, the sequences with the longest pieces first: one that began last would be waited for
-// (128 sequences of 1024 to 8192 keys: 170 us, in the order of the batch 200; 512 pieces and items 170, 640 176, 768 177).
+// (128 sequences of 1024 to 8192 keys: 173 us, in the order of the batch 203; 768 pieces and items 182).
 //
-// FEW (up to 64 sequences): lengths stay in registers.  Without it the same calls take 0.5 to 1.6 us longer, with its code for more rounds unrolled as much.
+// FEW (up to 64 sequences): lengths stay in registers (16 sequences 26.6 us, by the general variant 28.8, whose code is longer and cold).
 template <bool FEW>
 __device__ __forceinline__ bool q4_find(const AttnParams& p, const Q4Sched& sc, int w, int4* kept, Q4Piece& out) {
   const int lane = threadIdx.x & 63;
@@ -397,7 +397,7 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
   b += (slot - (b - first)) & (KS - 1);
   RowWindow win = row_window(nr, s);
   if (!row_on) win = RowWindow{0, 0, 0};
-  // a block that none of the wave's rows sees is passed over (2 sequences of 16 verify rows and 16 mask blocks of 16, where a row sees one: 66.2 -> 62.2 us)
+  // a block that none of the wave's rows sees is passed over (2 sequences of 16 verify rows and 16 mask blocks of 16, where a row sees one: 64.6 us, else 74.8)
   auto seen_from = [&](int b) FD_INLINE {
     while (b < last) {
       const int t0 = 32 * (b - cached);
@@ -659,7 +659,7 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
 
 // Merge of the partials of split items, by rows: a row is taken by TPR = DH / 8 lanes, eight channels each.  AT_ONCE pieces at a time, lane j of them
 // knows the maximum and sum of piece j; their values are requested with those, so that a batch is one latency.  Where an item may have many pieces,
-// 2^group_shift such groups of lanes share a row's and meet in LDS (1 sequence of 32 768 keys, 64 pieces an item: 27 us a call, without 47).
+// 2^group_shift such groups of lanes share a row's and meet in LDS (1 sequence of 32 768 keys: 24.4 us a call, with one group 33.1).
 template <int DH>
 __global__ __launch_bounds__(256) void attn_q4_combine_kernel(AttnParams p, Q4Sched sc, int group_shift) {
   typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
@@ -792,8 +792,8 @@ hipError_t run_attn_q4(const AttnParams& p, const Q4Cache& c, void* workspace, i
   char* ws = reinterpret_cast<char*>(workspace);
   const Q4Sched sc = {z.fixed, z.fixed > 0 ? 1.f / (float)z.fixed : 0.f, z.unit_shift, z.rt_max, (int)z.partials, reinterpret_cast<unsigned short*>(ws), reinterpret_cast<float*>(ws + z.off_ml), reinterpret_cast<int2*>(ws + z.off_entries)};
   if (z.wgs == 0) return hipSuccess;
-  // Pieces of an item, if the call's items are about equal: four of them to a group of lanes, so that twice as many are one batch (64 items of 4096 to
-  // 8192 keys 31.0 us a call, with eight 31.7, with two 31.0; 144 items of 272 rows 61.6, 61.7, 63.6).
+  // Pieces of an item, if the call's items are about equal: four of them to a group of lanes, so that twice as many are one batch (eight: the same within
+  // 1%; two: 2 sequences of 272 rows 64.6 -> 66.4 us).
   const int sets = 256 / (p.D / 8), most_rows = (int)((long long)p.max_new_rows * p.G < Q4_ROWS ? p.max_new_rows * p.G : Q4_ROWS);
   const long long pieces = z.fixed > 0 ? z.max_pieces : z.max_pieces < Q4_SLOTS / z.items ? z.max_pieces : Q4_SLOTS / z.items;
   int group_shift = 0;
