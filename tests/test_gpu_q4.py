@@ -216,6 +216,13 @@ def test_batches(fd, B, hkv):
     assert int(call.status.item()) == 0
 
 
+@pytest.mark.parametrize("dim,hq,ps", [(128, 8, 16), (64, 8, 48), (128, 2, 32)])
+def test_long_pieces(fd, dim, hq, ps):
+    """More blocks of a wave than lanes that know where they lie, also where the piece ends in the middle of a page."""
+    call = Q4Call(fd, kv=[9001, 2049], k=[8, 3], m=[8, 5], hq=hq, hkv=1, dim=dim, ps=ps, seed=31).upload(kv_chunk=8192)
+    call.check(*call.run())
+
+
 def test_scale_and_sharp_scores(fd):
     """Scores that spread over some hundred units of base 2: the running maximum moves often."""
     call = Q4Call(fd, kv=[400, 900], k=[4, 4], m=[4, 4], std=6.0, seed=8).upload(sm_scale=0.3)
