@@ -430,8 +430,8 @@ typedef struct fd_q4_cache {
  * fd_verify_draft_attn over a cache in 4 bits: the same operation, rows, masks, page lists, outputs and status bits.
  * args->k_cache, v_cache and the cache strides are not used; dtype (of q, k_new, v_new and out) is FD_BF16, head_dim 128 or 64,
  * page_size a multiple of 16.  The step's own rows take part in bf16, as they are.  FD_ATTN_PLANNED is
- * ignored (there is nothing to plan), FD_ATTN_FORCE_GENERIC refused.  kv_chunk > 0 (a multiple of 64) is the number of keys
- * of one sequence and head that a work-group takes.  Workspace: fd_verify_draft_attn_q4_workspace(args) bytes, device,
+ * ignored (there is nothing to plan), FD_ATTN_FORCE_GENERIC refused.  kv_chunk > 0 (a multiple of 64) is about the number of keys
+ * of one sequence and head that a work-group takes (own rows count more, and pieces of an item are equal).  Workspace: fd_verify_draft_attn_q4_workspace(args) bytes, device,
  * 256-byte aligned; nothing in it has to start at zero or survive a call, and calls that may overlap need one each.
  * Asynchronous on hip_stream.  Errors: FD_ERR_INVALID_ARG, FD_ERR_UNSUPPORTED, FD_ERR_WORKSPACE_TOO_SMALL, FD_ERR_HIP.
  */
