@@ -345,8 +345,8 @@ typedef struct fd_table_args {
   int32_t page_size;          /* tokens per page, >= 1                                        */
   int32_t table_stride;       /* entries per row of block_table, <= 2^20                      */
   int32_t total_rows;         /* entries of positions and slot_map, <= 2^20: rows past them are dropped (FD_DEV_ROWS_RANGE) */
-  int32_t page_indices_len;   /* entries of page_indices: lists end there (FD_DEV_PAGE_RANGE) */
-  int32_t free_pages_len;     /* entries of free_pages: pages given back past them are lost (FD_DEV_PAGE_RANGE) */
+  int32_t page_indices_len;   /* entries of page_indices, < 2^30: lists end there (FD_DEV_PAGE_RANGE) */
+  int32_t free_pages_len;     /* entries of free_pages, < 2^30: pages given back past them are lost (FD_DEV_PAGE_RANGE) */
   const int32_t *kv_len;      /* device [B]                                                   */
   const int32_t *verify_len;  /* device [B]                                                   */
   const int32_t *mask_rows;   /* device [B] or NULL (=> 0)                                    */

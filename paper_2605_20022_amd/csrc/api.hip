@@ -484,7 +484,9 @@ fd_status fd_step_tables(const fd_table_args* a, void* hip_stream) {
   if (a->page_size <= 0) return fail(FD_ERR_INVALID_ARG, "page_size %d must be positive", a->page_size);
   if (a->batch > 65535) return fail(FD_ERR_UNSUPPORTED, "batch %d > 65535", a->batch);
   if (a->table_stride > (1 << 20) || a->total_rows > (1 << 20)) return fail(FD_ERR_UNSUPPORTED, "table_stride %d / total_rows %d above 2^20", a->table_stride, a->total_rows);
-  if (a->page_indices_len > (1 << 30) || a->free_pages_len > (1 << 30)) return fail(FD_ERR_UNSUPPORTED, "page_indices_len / free_pages_len above 2^30");
+  // (the kernel adds up to 2^30, what 1024 requests of 2^20 entries come to, to a number of entries: below 2^30 of them no sum leaves 32 bits)
+  if (a->page_indices_len >= (1 << 30) || a->free_pages_len >= (1 << 30))
+    return fail(FD_ERR_UNSUPPORTED, "page_indices_len %d / free_pages_len %d of 2^30 or more", a->page_indices_len, a->free_pages_len);
   if (!a->row_indptr || !a->page_indptr || !a->free_count || !a->free_count_out ||
       (a->batch > 0 && (!a->kv_len || !a->verify_len || !a->table_len || !a->table_len_out)))
     return fail(FD_ERR_INVALID_ARG, "a required device pointer is NULL");

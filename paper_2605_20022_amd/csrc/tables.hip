@@ -31,7 +31,8 @@ __device__ __forceinline__ Request load_request(const fd_table_args& a, int i) {
   return r;
 }
 
-// Exclusive prefixes over the work-group and totals of N numbers a thread, in one trip through LDS.  Each is at most 2^20, so 1024 of them fit.
+// Exclusive prefixes over the work-group and totals of N numbers a thread, in one trip through LDS.  Each is at most 2^20, so 1024 of them sum to
+// 2^30 at most, and with the entries of an array (fewer than 2^30) or the rows (2^20) on top to less than 2^31.
 template <int N>
 __device__ __forceinline__ void block_excl_scan(const int (&x)[N], int (&before)[N], int (&total)[N], int (*sums)[TB_WAVES]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
