@@ -2,7 +2,7 @@
 //
 // An item is one (sequence, KV head, up to 128 tile rows); a tile row is (new row, query head of the group).  Its keys,
 // cached ones and then the sequence's own new rows, form blocks of 32.  Items are cut into pieces of about equal time, one per
-// work-group; an item of several pieces leaves (maximum, sum, un-normalised O) partials for the combine kernel.
+// work-group; an item of several pieces leaves (maximum, sum, un-normalised O) partials for the combine kernel, in fp32.
 //
 // A wave takes 32 tile rows and a stream of blocks, by itself: with up to 32 tile rows the four waves of a work-group
 // take every fourth block, with up to 64 two waves a row block take every second, else each wave has its own rows and all blocks.
@@ -49,8 +49,8 @@ struct Q4Sched {
   int unit_shift;           // work is counted in 2^unit_shift units
   int rt_max;               // items of a (sequence, head), at most
   int max_partials;         // partial slots in the workspace
-  unsigned short* part_acc; // [max_partials][128][D] fp16: the un-normalised O row divided by its largest magnitude
-  float* part_ml;           // [max_partials][128][4] maximum (base 2), sum, that largest magnitude, unused
+  float* part_acc;          // [max_partials][128][D] the un-normalised O row
+  float* part_ml;           // [max_partials][128][2] maximum (base 2), sum
   int2* entries;            // [B * Hkv * rt_max]: pieces, first partial slot
 };
 
@@ -233,11 +233,6 @@ __device__ __forceinline__ bf16x8 as_bf16x8(u32x4 x) { return __builtin_bit_cast
 __device__ __forceinline__ unsigned pack_bf16x2(float lo, float hi) {
   const f32x2 f = {lo, hi};
   return __builtin_bit_cast(unsigned, __builtin_convertvector(f, bf16x2));      // round to nearest even
-}
-__device__ __forceinline__ unsigned pack_f16x2(float lo, float hi) {
-  typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
-  const f32x2 f = {lo, hi};
-  return __builtin_bit_cast(unsigned, __builtin_convertvector(f, f16x2));
 }
 // The larger of a lane's value and that of lane ^ 32.
 __device__ __forceinline__ float max_halves(float x) {
@@ -626,23 +621,13 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
     if (pc.pieces > 1) {
       if (pc.slot + pc.piece >= sc.max_partials) continue;           // (only where the device's rows contradict the host's bounds)
       const long long at = (long long)(pc.slot + pc.piece) * Q4_ROWS + r;
-      float big = 0.f;
+      // In fp32: a row is a sum, whose channels may be of any size beside each other.  (As fp16 over the row's largest entry it would be half the bytes, 2
+      // sequences of 272 rows 64.3 us a call instead of 68.2, 1 of 16 rows 15.1 instead of 15.5; but what is 2^-16 of that entry loses its digits, and beside
+      // an infinity there is no largest entry.)
+      f32x4* dst = reinterpret_cast<f32x4*>(sc.part_acc + at * DH + part * CPT);
 #pragma unroll
-      for (int e = 0; e < CPT; ++e) big = fmaxf(big, fabsf(acc[e]));
-#pragma unroll
-      for (int d = 1; d < TPR; d <<= 1) big = fmaxf(big, __shfl_xor(big, d));
-      // fp16 relative to the row's largest magnitude: off by 2^-12 of it, where the result's own rounding is 2^-8 of its value.  A row with an infinity
-      // or a NaN (fmaxf does not see one) keeps both: they are their own fp16.  (A reciprocal that is no number: the row stays fp32's subnormals, zeros.)
-      const bool scaled = big > 1e-37f && big < INFINITY;
-      const float inv = scaled ? 1.f / big : 1.f;
-      unsigned* dst = reinterpret_cast<unsigned*>(sc.part_acc + at * DH + part * CPT);
-      u32x4 w;
-#pragma unroll
-      for (int e = 0; e < CPT; e += 2) {
-        w[e / 2 % 4] = pack_f16x2(acc[e] * inv, acc[e + 1] * inv);
-        if (e % 8 == 6) *reinterpret_cast<u32x4*>(dst + e / 8 * 4) = w;
-      }
-      if (part == 0) *reinterpret_cast<f32x4*>(sc.part_ml + at * 4) = f32x4{M, sum, scaled ? big : 1.f, 0.f};
+      for (int e = 0; e < CPT; e += 4) dst[e / 4] = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
+      if (part == 0) *reinterpret_cast<f32x2*>(sc.part_ml + at * 2) = f32x2{M, sum};
     } else {
       const int t = pc.rt * Q4_ROWS + r, n = t / p.G;
       const long long orow = (long long)(s.row0 + n) * p.Hq + pc.head * p.G + (t - n * p.G);
@@ -662,7 +647,6 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
 // 2^group_shift such groups of lanes share a row's and meet in LDS (1 sequence of 32 768 keys: 24.4 us a call, with one group 33.1).
 template <int DH>
 __global__ __launch_bounds__(256) void attn_q4_combine_kernel(AttnParams p, Q4Sched sc, int group_shift) {
-  typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
   constexpr int TPR = DH / 8, SETS = 256 / TPR, AT_ONCE = 8;
   __shared__ float lds_acc[SETS][DH + 4], lds_ml[SETS][2];
   const int item = blockIdx.x, rt = item % sc.rt_max, head = item / sc.rt_max % p.Hkv, seq = item / sc.rt_max / p.Hkv;
@@ -683,11 +667,14 @@ __global__ __launch_bounds__(256) void attn_q4_combine_kernel(AttnParams p, Q4Sc
     const int q = q0 + group * AT_ONCE, n = min(AT_ONCE, pieces - q);
     if (n <= 0) break;                                   // (the same for all lanes of a set)
     const long long at = (long long)(slot + q) * Q4_ROWS + rr;
-    f32x4 ml = {-3e38f, 0.f, 0.f, 0.f};
-    if (j < n) ml = *reinterpret_cast<const f32x4*>(sc.part_ml + (at + (long long)j * Q4_ROWS) * 4);
-    u32x4 w[AT_ONCE];
+    f32x2 ml = {-3e38f, 0.f};
+    if (j < n) ml = *reinterpret_cast<const f32x2*>(sc.part_ml + (at + (long long)j * Q4_ROWS) * 2);
+    f32x4 w[AT_ONCE][2];
 #pragma unroll
-    for (int u = 0; u < AT_ONCE; ++u) w[u] = *reinterpret_cast<const u32x4*>(sc.part_acc + (at + (long long)min(u, n - 1) * Q4_ROWS) * DH + part * 8);
+    for (int u = 0; u < AT_ONCE; ++u) {
+      const f32x4* src = reinterpret_cast<const f32x4*>(sc.part_acc + (at + (long long)min(u, n - 1) * Q4_ROWS) * DH + part * 8);
+      w[u][0] = src[0]; w[u][1] = src[1];
+    }
     float top = ml[0];
 #pragma unroll
     for (int d = 1; d < AT_ONCE; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
@@ -696,7 +683,6 @@ __global__ __launch_bounds__(256) void attn_q4_combine_kernel(AttnParams p, Q4Sc
     float add = f * ml[1];
 #pragma unroll
     for (int d = 1; d < AT_ONCE; d <<= 1) add += __shfl_xor(add, d);
-    const float weight = f * ml[2];
     M = mn;
     sum = sum * shrink + add;
 #pragma unroll
@@ -704,10 +690,9 @@ __global__ __launch_bounds__(256) void attn_q4_combine_kernel(AttnParams p, Q4Sc
 #pragma unroll
     for (int u = 0; u < AT_ONCE; ++u) {
       if (u >= n) break;                                 // (no zero times an infinity)
-      const float g = __shfl(weight, lane0 + u);
-      const f16x8 v = __builtin_bit_cast(f16x8, w[u]);
+      const float g = __shfl(f, lane0 + u);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) acc[k] += g * (float)v[k];
+      for (int k = 0; k < 8; ++k) acc[k] += g * w[u][k / 4][k % 4];
     }
   }
   if (group_shift > 0) {
@@ -774,8 +759,8 @@ static Q4Shape q4_shape(int batch, int num_kv_heads, int group, int total_rows, 
     if (most < z.partials) z.partials = most;
   }
   auto round = [](size_t x) { return (x + 255) / 256 * 256; };
-  z.off_ml = round((size_t)z.partials * Q4_ROWS * head_dim * sizeof(unsigned short));
-  z.off_entries = z.off_ml + round((size_t)z.partials * Q4_ROWS * 4 * sizeof(float));
+  z.off_ml = round((size_t)z.partials * Q4_ROWS * head_dim * sizeof(float));
+  z.off_entries = z.off_ml + round((size_t)z.partials * Q4_ROWS * 2 * sizeof(float));
   z.total = z.off_entries + round((size_t)(batch > 0 ? batch : 1) * num_kv_heads * z.rt_max * sizeof(int2));
   return z;
 }
@@ -790,7 +775,7 @@ size_t attn_q4_workspace(int batch, int num_kv_heads, int group, int total_rows,
 hipError_t run_attn_q4(const AttnParams& p, const Q4Cache& c, void* workspace, int kv_chunk, hipStream_t st) {
   const Q4Shape z = q4_shape(p.B, p.Hkv, p.G, p.total_rows, p.max_kv_len, p.max_new_rows, kv_chunk, p.D);
   char* ws = reinterpret_cast<char*>(workspace);
-  const Q4Sched sc = {z.fixed, z.fixed > 0 ? 1.f / (float)z.fixed : 0.f, z.unit_shift, z.rt_max, (int)z.partials, reinterpret_cast<unsigned short*>(ws), reinterpret_cast<float*>(ws + z.off_ml), reinterpret_cast<int2*>(ws + z.off_entries)};
+  const Q4Sched sc = {z.fixed, z.fixed > 0 ? 1.f / (float)z.fixed : 0.f, z.unit_shift, z.rt_max, (int)z.partials, reinterpret_cast<float*>(ws), reinterpret_cast<float*>(ws + z.off_ml), reinterpret_cast<int2*>(ws + z.off_entries)};
   if (z.wgs == 0) return hipSuccess;
   // Pieces of an item, if the call's items are about equal: four of them to a group of lanes, so that twice as many are one batch (eight: the same within
   // 1%; two: 2 sequences of 272 rows 64.6 -> 66.4 us).
