@@ -22,26 +22,14 @@
 // the same arithmetic leaves little time: 128 sequences of 1024 to 8192 keys, up to 16 rows 173 us, 3.9 TB/s.  One short sequence is latency
 // (15.2 us): lengths, pages, codes, merge, second launch.
 #include "kv_q4.h"
+#include "q4_shape.h"
 
 namespace fd {
 
 #define FD_INLINE __attribute__((always_inline))      // on a lambda: what it captures stays in registers
 
 constexpr int Q4_BLOCK = 256;
-constexpr int Q4_TK = 32;                 // keys of a block
-constexpr int Q4_ROWS = 128;              // tile rows of an item
 constexpr float Q4_LAZY = 256.f;          // sum of a row's sixteen probabilities from which on the softmax reference follows the row maximum
-constexpr int Q4_SLOTS = 512;             // work-groups that run at once: two a compute unit
-// Units a compute unit up to which it takes one piece (one sequence of 32 768 keys, 64 rows, 99 units: 24.4 us a call, in twice as many pieces 27.4;
-// 4 of 8192 to 16 384, 146: 30.4 and 32.1; one of 8192, 272 rows, 420: 56.8 and 54.5).
-constexpr int Q4_ALONE = 192;
-constexpr int Q4_PIECES = 512;            // pieces aimed at where there are Q4_SLOTS items or more
-constexpr int Q4_CLASSES = 4;             // lengths of pieces that are told apart
-// A block of own rows takes as long as Q4_OWN of cached ones, the first Q4_OWN_START more (1 sequence of 16 new rows 15.1 us a call, 2 of 272 in 17
-// blocks 64.5; counted as cached ones 16.6 and 66.4, with 6 more 15.2 and 66.0).
-constexpr int Q4_OWN = 3, Q4_OWN_START = 4;
-constexpr int Q4_MIN_PIECE = 8;           // blocks of a piece, at least, but for the last of a short item (1 sequence of 1024 keys 14.1 us; 6: 14.8, 12: 14.6)
-constexpr int Q4_KEPT = 4;                // rounds of 64 sequences whose lengths a wave keeps in LDS
 
 struct Q4Sched {
   int fixed;                // > 0: blocks of a piece, asked for by the caller
@@ -726,43 +714,6 @@ __global__ __launch_bounds__(256) void attn_q4_combine_kernel(AttnParams p, Q4Sc
   for (int u = 0; u < 4; ++u) w[u] = pack_bf16x2(acc[2 * u] * inv, acc[2 * u + 1] * inv);
   *reinterpret_cast<u32x4*>(reinterpret_cast<bf16_t*>(p.out) + orow * DH + part * 8) = w;
   if (part == 0 && p.lse) p.lse[orow] = (M + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
-}
-
-// Items of the largest sequence, partial slots and work-groups that there can be, and the workspace.
-struct Q4Shape { long long items, partials, wgs, max_pieces; int rt_max, fixed, unit_shift; size_t off_ml, off_entries, total; };
-static Q4Shape q4_shape(int batch, int num_kv_heads, int group, int total_rows, int max_kv_len, int max_new_rows, int kv_chunk, int head_dim) {
-  Q4Shape z;
-  const long long tile_rows = (long long)max_new_rows * group;
-  z.rt_max = (int)((tile_rows + Q4_ROWS - 1) / Q4_ROWS);
-  if (z.rt_max < 1) z.rt_max = 1;
-  z.fixed = kv_chunk / Q4_TK;
-  const long long seqs = batch < total_rows ? batch : total_rows;       // sequences that have rows
-  z.items = seqs * num_kv_heads * z.rt_max;
-  const long long blocks = ((long long)max_kv_len + Q4_TK - 1) / Q4_TK + Q4_OWN_START + Q4_OWN * ((max_new_rows + Q4_TK - 1) / Q4_TK);
-  // units of all sequences' work: sequences whose rows add up to total_rows at most, every one as long as may be
-  const double units = ((double)total_rows * group / 32 + 2.0 * seqs) * 2 * (double)blocks;
-  z.unit_shift = 0;
-  while (units / (double)(1ll << z.unit_shift) >= 1073741824.0) ++z.unit_shift;
-  z.max_pieces = blocks / (z.fixed > 0 ? z.fixed : Q4_MIN_PIECE) + 1;
-  if (z.fixed > 0) {
-    z.wgs = z.items * z.max_pieces;
-    z.partials = z.wgs;
-  } else {
-    // pieces - 1 of an item are density x units at most, which sum to Q4_PIECES over all items (Q4_SLOTS in one round)
-    static_assert(Q4_SLOTS <= Q4_PIECES, "what one round takes is within the bounds of several");
-    // (work-groups without a piece are not free, 0.8 us for 528 of them: none where one round is sure to do)
-    const bool one_round = z.items < Q4_SLOTS && batch <= 64 * Q4_KEPT;
-    z.wgs = one_round ? Q4_SLOTS : z.items + Q4_PIECES;
-    z.partials = one_round ? Q4_SLOTS : 2 * Q4_PIECES;                  // an item in c >= 2 pieces: c <= 2 (c - 1)
-    const long long most = z.items * z.max_pieces;
-    if (most < z.wgs) z.wgs = most;
-    if (most < z.partials) z.partials = most;
-  }
-  auto round = [](size_t x) { return (x + 255) / 256 * 256; };
-  z.off_ml = round((size_t)z.partials * Q4_ROWS * head_dim * sizeof(float));
-  z.off_entries = z.off_ml + round((size_t)z.partials * Q4_ROWS * 2 * sizeof(float));
-  z.total = z.off_entries + round((size_t)(batch > 0 ? batch : 1) * num_kv_heads * z.rt_max * sizeof(int2));
-  return z;
 }
 
 // 0 where the call is too large for one launch (2^24 work-groups of 256 threads).

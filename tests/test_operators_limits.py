@@ -1,8 +1,10 @@
 """Limits of the calls around a 4-bit cache, on both sides, as far as the host decides them."""
+import os
+import subprocess
 
 import pytest
 
-from tests.test_operators_host import _refused, _tables
+from tests.test_operators_host import ROOT, _refused, _tables
 
 
 @pytest.mark.parametrize("entries", ["page_indices_len", "free_pages_len"])
@@ -12,3 +14,31 @@ def test_step_tables_sum_in_32_bits(entries):
         _refused(_tables(**{entries: n}), 2, "2^30")
     # one fewer is taken: the next check has its turn
     _refused(_tables(**{entries: (1 << 30) - 1, "kv_len": None}), 1, "NULL")
+
+
+def _weight(rows):
+    """How long a block takes a work-group with so many tile rows, in halves (attn_q4.hip)."""
+    return 0 if rows == 0 else 2 if rows <= 32 else 3 if rows <= 64 else 6
+
+
+def test_work_is_counted_in_32_bits_whatever_the_rows_on_the_device(tmp_path):
+    """The kernel sums the work of all sequences in units of 2^unit_shift.  Row offsets that overlap can give each of them max_new_rows rows, and the sum must
+    hold those too: from it follows how many pieces there are, and where their partial rows go."""
+    src = '''#include <stdio.h>
+#include "q4_shape.h"
+int main() { int a[8]; while (scanf("%d %d %d %d %d %d %d %d", a, a + 1, a + 2, a + 3, a + 4, a + 5, a + 6, a + 7) == 8)
+  printf("%d\\n", fd::q4_shape(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7]).unit_shift); }
+'''
+    (tmp_path / "t.cpp").write_text(src)
+    subprocess.check_call(["g++", "-std=c++17", "-Wall", "-Werror", "-I", os.path.join(ROOT, "paper_2605_20022_amd", "csrc"), str(tmp_path / "t.cpp"), "-o", str(tmp_path / "t")])
+    shapes = [(B, H, G, R, L, n, 0, 128) for B in (1, 16, 64, 65, 256, 1000, 65535) for H in (1, 8) for G in (1, 4, 16) for R in (1, 1000, 65536, 1 << 20)
+              for L in (0, 4096, 1 << 21, 1 << 30) for n in (1, 16, 272, 65536, 1 << 20) if n * G <= 1 << 24]
+    out = subprocess.run([str(tmp_path / "t")], input="\n".join(" ".join(map(str, s)) for s in shapes), capture_output=True, text=True, check=True).stdout.split()
+    assert len(out) == len(shapes)
+    for (B, H, G, R, L, n, *_), shift in zip(shapes, map(int, out)):
+        n = min(n, R)
+        blocks = -(-L // 32) + 4 + 3 * -(-n // 32)
+        units = blocks * (n * G // 128 * _weight(128) + _weight(n * G % 128))
+        assert B * -(-units // (1 << shift)) < 1 << 31, (B, H, G, R, L, n, shift)
+    # where the work is little, as in any ordinary call, it is counted as it is
+    assert {int(s) for (B, H, G, R, L, n, *_), s in zip(shapes, out) if B <= 256 and L <= 4096 and n <= 272} == {0}
