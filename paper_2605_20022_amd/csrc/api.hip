@@ -27,6 +27,7 @@ hipError_t run_qk_norm_rope(const fd_rope_args& a, hipStream_t st);
 size_t attn_q4_workspace(int batch, int num_kv_heads, int group, int total_rows, int max_kv_len, int max_new_rows, int kv_chunk, int head_dim);
 hipError_t run_attn_q4(const AttnParams& p, const Q4Cache& c, void* workspace, int kv_chunk, hipStream_t st);
 hipError_t run_append_kv_q4(const AttnParams& p, const Q4Cache& c, const int* accept_len, int* kv_len_out, hipStream_t st);
+long long read_kv_q4_wgs(int batch, int total_rows);
 hipError_t run_read_kv_q4(const Q4Cache& c, int batch, int num_kv_heads, int head_dim, int page_size, int num_pages, const int* page_indptr,
                           const int* page_indices, int page_entries, const int* start, const int* out_indptr, int total_rows, void* k_out,
                           void* v_out, int dtype, uint32_t* status, hipStream_t st);
@@ -653,6 +654,7 @@ fd_status fd_read_kv_q4(const fd_q4_cache* cache, int32_t batch, int32_t num_kv_
   if (st != FD_OK) return st;
   g_err[0] = 0;
   if (batch == 0 || total_rows == 0) return FD_OK;
+  if (fd::read_kv_q4_wgs(batch, total_rows) >= (1ll << 24)) return fail(FD_ERR_UNSUPPORTED, "total_rows %d too large for one launch", total_rows);
   if (!q4_cache_complete(cache) || !page_indptr || !page_indices || !out_indptr || !k_out || !v_out || num_pages == 0)
     return fail(FD_ERR_INVALID_ARG, "a required device pointer is NULL or num_pages is 0");
   if (!aligned16(k_out) || !aligned16(v_out)) return fail(FD_ERR_INVALID_ARG, "k_out and v_out must be 16-byte aligned");

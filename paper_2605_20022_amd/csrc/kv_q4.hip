@@ -264,10 +264,12 @@ __global__ __launch_bounds__(256) void read_kv_q4_kernel(ReadParams p, Q4Cache c
   }
 }
 
+// Work-groups of a head: 64 tokens each; a sequence begins with up to seven that are not asked for, and ends in part of 64.
+long long read_kv_q4_wgs(int batch, int total_rows) { return total_rows / AQ_TOKENS + 2ll * (batch < total_rows ? batch : total_rows); }
+
 template <typename T>
 static void launch_read(const ReadParams& p, const Q4Cache& c, int head_dim, void* k_out, void* v_out, hipStream_t st) {
-  // 64 tokens each; a sequence begins with up to seven that are not asked for, and ends in part of 64
-  const dim3 grid((unsigned)((long long)p.total_rows / AQ_TOKENS + 2ll * (p.B < p.total_rows ? p.B : p.total_rows)), p.Hkv);
+  const dim3 grid((unsigned)read_kv_q4_wgs(p.B, p.total_rows), p.Hkv);
   if (head_dim == 128) hipLaunchKernelGGL((read_kv_q4_kernel<128, T>), grid, dim3(256), 0, st, p, c, reinterpret_cast<T*>(k_out), reinterpret_cast<T*>(v_out));
   else hipLaunchKernelGGL((read_kv_q4_kernel<64, T>), grid, dim3(256), 0, st, p, c, reinterpret_cast<T*>(k_out), reinterpret_cast<T*>(v_out));
 }

@@ -1,10 +1,12 @@
 """Limits of the calls around a 4-bit cache, on both sides, as far as the host decides them."""
+import ctypes as C
 import os
 import subprocess
 
 import pytest
 
-from tests.test_operators_host import ROOT, _refused, _tables
+from paper_2605_20022_amd import flexdraft as fd
+from tests.test_operators_host import P, ROOT, _cache, _refused, _tables
 
 
 @pytest.mark.parametrize("entries", ["page_indices_len", "free_pages_len"])
@@ -42,3 +44,17 @@ int main() { int a[8]; while (scanf("%d %d %d %d %d %d %d %d", a, a + 1, a + 2, 
         assert B * -(-units // (1 << shift)) < 1 << 31, (B, H, G, R, L, n, shift)
     # where the work is little, as in any ordinary call, it is counted as it is
     assert {int(s) for (B, H, G, R, L, n, *_), s in zip(shapes, out) if B <= 256 and L <= 4096 and n <= 272} == {0}
+
+
+def _read(total_rows, batch=2, **kw):
+    a = dict(page_indptr=P, page_indices=P, out_indptr=P, k_out=P, v_out=P)
+    a.update(kw)
+    return fd.load().fd_read_kv_q4(C.byref(_cache()), batch, 8, 128, 16, 10, a["page_indptr"], a["page_indices"], 20, None, a["out_indptr"], total_rows, a["k_out"],
+                                   a["v_out"], fd.FD_F32, None, None)
+
+
+def test_read_back_of_too_many_rows_for_a_launch():
+    """2^24 work-groups of 256 threads, 64 rows each and up to two more a sequence."""
+    for rows, batch in ((1 << 30, 1), ((1 << 31) - 1, 65535), ((1 << 30) - 64 * 4, 2)):
+        _refused(_read(rows, batch), 2, "too large")
+    _refused(_read((1 << 30) - 64 * 4 - 1, 2, v_out=None), 1, "NULL")
