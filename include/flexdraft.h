@@ -451,7 +451,7 @@ FD_API fd_status fd_append_kv_q4(const fd_attn_args *args, const fd_q4_cache *ca
  * out_indptr[i] .. of k_out and v_out, [total_rows][num_kv_heads][head_dim] dense, FD_F32 (exactly the values) or FD_BF16
  * (values rounded).  Tokens that the page list has no place for leave their rows as they were (FD_DEV_PAGE_RANGE).
  *   start       device int32 [B] or NULL (=> 0)
- *   out_indptr  device int32 [B+1]
+ *   out_indptr  device int32 [B+1], not decreasing, up to total_rows (else FD_DEV_ROWS_RANGE)
  *   total_rows  rows of k_out and v_out: total_rows + 128 * min(B, total_rows) < 2^30 (one launch)
  *   status      device uint32[1] or NULL
  * Asynchronous on hip_stream.  Errors: FD_ERR_INVALID_ARG, FD_ERR_UNSUPPORTED, FD_ERR_HIP.

@@ -186,8 +186,11 @@ __global__ __launch_bounds__(256) void read_kv_q4_kernel(ReadParams p, Q4Cache c
     const int i = c0 + lane;
     int a = 0, rows = 0, st = 0, chunks = 0;
     if (i < p.B) {
-      a = clampi(p.out_indptr[i], 0, p.total_rows);
-      rows = clampi(p.out_indptr[i + 1], 0, p.total_rows) - a;
+      const int r0 = p.out_indptr[i], r1 = p.out_indptr[i + 1];
+      // (The last work-group comes by every sequence, or stops behind offsets that decrease: without those it has tokens only where there is one sequence.)
+      if (blockIdx.x == gridDim.x - 1 && head == 0 && tid < 64 && (r0 < 0 || r1 < r0 || r1 > p.total_rows)) flag_status(p.status, FD_DEV_ROWS_RANGE);
+      a = clampi(r0, 0, p.total_rows);
+      rows = clampi(r1, 0, p.total_rows) - a;
       st = p.start ? p.start[i] : 0;
       if (rows > 0) chunks = ((st & 7) + rows + AQ_TOKENS - 1) / AQ_TOKENS;
     }
