@@ -156,7 +156,7 @@ hipError_t run_append_kv_q4(const AttnParams& p, const Q4Cache& c, const int* ac
 
 // ---- read-back --------------------------------------------------------------------------------
 struct ReadParams {
-  int B, Hkv, page_size, num_pages, page_entries, total_rows;
+  int B, Hkv, page_size, num_pages, page_entries, total_rows, last_wg;
   const int* page_indptr; const int* page_indices; const int* start; const int* out_indptr;
   uint32_t* status;
 };
@@ -186,11 +186,8 @@ __global__ __launch_bounds__(256) void read_kv_q4_kernel(ReadParams p, Q4Cache c
     const int i = c0 + lane;
     int a = 0, rows = 0, st = 0, chunks = 0;
     if (i < p.B) {
-      const int r0 = p.out_indptr[i], r1 = p.out_indptr[i + 1];
-      // (The last work-group comes by every sequence, or stops behind offsets that decrease: without those it has tokens only where there is one sequence.)
-      if (blockIdx.x == gridDim.x - 1 && head == 0 && tid < 64 && (r0 < 0 || r1 < r0 || r1 > p.total_rows)) flag_status(p.status, FD_DEV_ROWS_RANGE);
-      a = clampi(r0, 0, p.total_rows);
-      rows = clampi(r1, 0, p.total_rows) - a;
+      a = clampi(p.out_indptr[i], 0, p.total_rows);
+      rows = clampi(p.out_indptr[i + 1], 0, p.total_rows) - a;
       st = p.start ? p.start[i] : 0;
       if (rows > 0) chunks = ((st & 7) + rows + AQ_TOKENS - 1) / AQ_TOKENS;
     }
@@ -204,6 +201,11 @@ __global__ __launch_bounds__(256) void read_kv_q4_kernel(ReadParams p, Q4Cache c
     }
     base = __builtin_amdgcn_readlane(incl, 63);
   }
+  if ((int)blockIdx.x == p.last_wg && head == 0)       // (it has seldom tokens to read)
+    for (int i = tid; i < p.B; i += 256) {
+      const int r0 = p.out_indptr[i], r1 = p.out_indptr[i + 1];
+      if (r0 < 0 || r1 < r0 || r1 > p.total_rows) flag_status(p.status, FD_DEV_ROWS_RANGE);
+    }
   if (seq < 0) return;
   const int pg0 = clampi(sload(p.page_indptr, seq), 0, p.page_entries), pg1 = clampi(sload(p.page_indptr, seq + 1), pg0, p.page_entries);
   const long long room = (long long)(pg1 - pg0) * p.page_size;
@@ -272,7 +274,7 @@ long long read_kv_q4_wgs(int batch, int total_rows) { return total_rows / AQ_TOK
 
 template <typename T>
 static void launch_read(const ReadParams& p, const Q4Cache& c, int head_dim, void* k_out, void* v_out, hipStream_t st) {
-  const dim3 grid((unsigned)read_kv_q4_wgs(p.B, p.total_rows), p.Hkv);
+  const dim3 grid(p.last_wg + 1, p.Hkv);
   if (head_dim == 128) hipLaunchKernelGGL((read_kv_q4_kernel<128, T>), grid, dim3(256), 0, st, p, c, reinterpret_cast<T*>(k_out), reinterpret_cast<T*>(v_out));
   else hipLaunchKernelGGL((read_kv_q4_kernel<64, T>), grid, dim3(256), 0, st, p, c, reinterpret_cast<T*>(k_out), reinterpret_cast<T*>(v_out));
 }
@@ -280,7 +282,8 @@ static void launch_read(const ReadParams& p, const Q4Cache& c, int head_dim, voi
 hipError_t run_read_kv_q4(const Q4Cache& c, int batch, int num_kv_heads, int head_dim, int page_size, int num_pages, const int* page_indptr,
                           const int* page_indices, int page_entries, const int* start, const int* out_indptr, int total_rows, void* k_out,
                           void* v_out, int dtype, uint32_t* status, hipStream_t st) {
-  const ReadParams p = {batch, num_kv_heads, page_size, num_pages, page_entries, total_rows, page_indptr, page_indices, start, out_indptr, status};
+  const ReadParams p = {batch, num_kv_heads, page_size, num_pages, page_entries, total_rows, (int)read_kv_q4_wgs(batch, total_rows) - 1, page_indptr,
+                        page_indices, start, out_indptr, status};
   if (dtype == FD_BF16) launch_read<bf16_t>(p, c, head_dim, k_out, v_out, st);
   else launch_read<float>(p, c, head_dim, k_out, v_out, st);
   return hipGetLastError();
