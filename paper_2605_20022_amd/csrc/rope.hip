@@ -16,6 +16,7 @@ template <typename T, int E> struct Piece;
 template <> struct Piece<bf16_t, 4> {
   u16x4 w;
   __device__ __forceinline__ void load(const bf16_t* p) { w = *reinterpret_cast<const u16x4*>(p); }
+  __device__ __forceinline__ void copy(bf16_t* p) const { *reinterpret_cast<u16x4*>(p) = w; }
   __device__ __forceinline__ void get(float (&x)[4]) const {
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] = bf16_to_f32(w[e]);
@@ -30,6 +31,7 @@ template <> struct Piece<bf16_t, 4> {
 template <> struct Piece<bf16_t, 8> {
   u32x4 w;
   __device__ __forceinline__ void load(const bf16_t* p) { w = *reinterpret_cast<const u32x4*>(p); }
+  __device__ __forceinline__ void copy(bf16_t* p) const { *reinterpret_cast<u32x4*>(p) = w; }
   __device__ __forceinline__ void get(float (&x)[8]) const {
 #pragma unroll
     for (int e = 0; e < 4; ++e) { x[2 * e] = __uint_as_float(w[e] << 16); x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u); }
@@ -49,6 +51,7 @@ template <> struct Piece<bf16_t, 8> {
 template <> struct Piece<float, 4> {
   f32x4 w;
   __device__ __forceinline__ void load(const float* p) { w = *reinterpret_cast<const f32x4*>(p); }
+  __device__ __forceinline__ void copy(float* p) const { *reinterpret_cast<f32x4*>(p) = w; }
   __device__ __forceinline__ void get(float (&x)[4]) const {
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] = w[e];
@@ -158,7 +161,12 @@ __global__ __launch_bounds__(RP_WAVES * 64) void qk_norm_rope_kernel(fd_rope_arg
     T* dst;
     if (is_q) dst = reinterpret_cast<T*>(a.q_out) + ((long long)row * Hq + h) * D;
     else if (!is_v) dst = reinterpret_cast<T*>(a.k_out) + ((long long)row * Hkv + h - Hq) * D;
-    else dst = reinterpret_cast<T*>(a.v_out) + ((long long)row * Hkv + h - Hq - Hkv) * D;
+    else {                                               // bit by bit: a conversion makes a signalling NaN a quiet one
+      dst = reinterpret_cast<T*>(a.v_out) + ((long long)row * Hkv + h - Hq - Hkv) * D;
+      w[0].copy(dst + e0);
+      w[1].copy(dst + e1);
+      return;
+    }
     P::store(dst + e0, x);
     P::store(dst + e1, y);
   };
