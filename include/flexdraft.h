@@ -416,7 +416,10 @@ FD_API fd_status fd_qk_norm_rope(const fd_rope_args *args, void *hip_stream);
  *           v_scales  [page][head][slot] bf16
  * 134 bytes a token and head at D = 128, where bf16 takes 512.  A group of keys, or a token's values, that holds an infinity or
  * a NaN is stored as NaN.  D is 128 or 64, page_size a multiple of 16.  The block (page p, head g) of each array is number
- * p * stride_page + g * stride_head (dense: num_kv_heads and 1).
+ * p * stride_page + g * stride_head (dense: num_kv_heads and 1).  Slots are numbered in 32 bits over all blocks, those that the strides
+ * leave out included: page_size * ((num_pages - 1) * stride_page + (num_kv_heads - 1) * stride_head + 1) <= 2^32 (else FD_ERR_UNSUPPORTED).
+ * A pool that several layers share with their heads between a page's others has stride_page = layers * num_kv_heads, and this
+ * limit for all of them together; layers that follow each other have it for each.
  */
 typedef struct fd_q4_cache {
   void *k_codes;              /* device, 16-byte aligned                                      */

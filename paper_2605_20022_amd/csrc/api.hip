@@ -535,9 +535,10 @@ static fd_status check_q4_cache(const fd_q4_cache* c, int head_dim, int page_siz
   if (num_kv_heads <= 0 || num_kv_heads > 65535) return fail(FD_ERR_INVALID_ARG, "num_kv_heads %d", num_kv_heads);
   if (c->stride_page < 0 || c->stride_head < 0 || c->stride_page >= (1ll << 31) || c->stride_head >= (1ll << 31))
     return fail(FD_ERR_INVALID_ARG, "cache strides must be in [0, 2^31) blocks");
-  // tokens are numbered in 32 bits (an array of 2^32 of them takes more memory than there is)
+  // The attention numbers slots in 32 bits, over all blocks between the first and the last that is used, gaps included (2^32 of them without
+  // gaps take 292 GB at head dim 64, 575 GB at 128).
   if ((double)page_size * ((double)(num_pages > 0 ? num_pages - 1 : 0) * c->stride_page + (double)(num_kv_heads - 1) * c->stride_head + 1.0) > 4294967296.0)
-    return fail(FD_ERR_UNSUPPORTED, "a cache of more than 2^32 tokens and heads");
+    return fail(FD_ERR_UNSUPPORTED, "a cache whose blocks span more than 2^32 slots");
   if (!aligned16(c->k_codes) || !aligned16(c->v_codes) || !aligned16(c->v_scales) || (reinterpret_cast<uintptr_t>(c->k_scales) & 3))
     return fail(FD_ERR_INVALID_ARG, "k_codes, v_codes and v_scales must be 16-byte aligned, k_scales 4-byte aligned");
   return FD_OK;

@@ -6,7 +6,7 @@ import subprocess
 import pytest
 
 from paper_2605_20022_amd import flexdraft as fd
-from tests.test_operators_host import P, ROOT, _cache, _refused, _tables
+from tests.test_operators_host import P, ROOT, _attn, _cache, _refused, _tables
 
 
 @pytest.mark.parametrize("entries", ["page_indices_len", "free_pages_len"])
@@ -58,3 +58,19 @@ def test_read_back_of_too_many_rows_for_a_launch():
     for rows, batch in ((1 << 30, 1), ((1 << 31) - 1, 65535), ((1 << 30) - 64 * 4, 2)):
         _refused(_read(rows, batch), 2, "too large")
     _refused(_read((1 << 30) - 64 * 4 - 1, 2, v_out=None), 1, "NULL")
+
+
+@pytest.mark.parametrize("page_size,pages,heads,stride_page,stride_head", [(16, (1 << 25) + 1, 8, 8, 1), (32, 1 << 24, 8, 8, 1), (16, 1 << 25, 8, 8, 1),
+                                                                           (16, (1 << 28) - 7, 1, 1, 1), (16, 64, 4, 1, 1 << 24), (16, 3, 8, 64 * (1 << 20), 1),
+                                                                           (16, 1 << 19, 8, 512, 1), (16, (1 << 19) + 1, 8, 512, 1)])
+def test_slots_are_numbered_in_32_bits(page_size, pages, heads, stride_page, stride_head):
+    """On both sides of 2^32 slots, and with strides that leave blocks out (a pool that 64 layers share)."""
+    fits = page_size * ((pages - 1) * stride_page + (heads - 1) * stride_head + 1) <= 1 << 32
+    cache = _cache(stride_page=stride_page, stride_head=stride_head)
+    args = dict(page_size=page_size, num_pages=pages, num_kv_heads=heads, num_q_heads=heads * 4)
+    a, b = _attn(**dict(args, workspace=None)), _attn(**dict(args, k_new=None))
+    calls = [fd.load().fd_verify_draft_attn_q4(C.byref(a), C.byref(cache), None), fd.load().fd_append_kv_q4(C.byref(b), C.byref(cache), P, P, None),
+             fd.load().fd_read_kv_q4(C.byref(cache), 2, heads, 128, page_size, pages, P, P, 20, None, P, 5, None, P, fd.FD_F32, None, None)]
+    assert calls == ([1, 1, 1] if fits else [2, 2, 2])            # (what fits: the missing pointer has its turn)
+    if not fits:
+        assert b"2^32" in fd.load().fd_last_error()
