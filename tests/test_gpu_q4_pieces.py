@@ -51,3 +51,64 @@ def test_small_channels_beside_a_large_one(fd, dim, kv_chunk):
     call.v_new = bits_of(v)
     out, _ = call.upload(kv_chunk=kv_chunk).run()
     assert_rows_hold(call, out)
+
+
+# ---- how items are cut ------------------------------------------------------------------------
+ROUND = 512                       # work-groups that run at once
+
+
+def items_of(call, hkv):
+    """Items of the call: up to 128 tile rows of a sequence and KV head each."""
+    group = call.q.shape[1] // hkv
+    return hkv * int((-(-call.n * group // 128)).sum())
+
+
+@pytest.mark.parametrize("B,hkv,dim", [(64, 8, 128), (64, 9, 64), (65, 8, 128), (130, 4, 128), (200, 3, 64), (256, 2, 128)])
+def test_more_items_than_run_at_once(fd, B, hkv, dim):
+    """As many items as work-groups run at once, or more, and no more sequences than a wave keeps the lengths of: sequences of very different length, taken the
+    longest pieces first, by the variant of up to 64 sequences and the other.  Every sequence has a row."""
+    rng = np.random.default_rng(B + hkv)
+    kv = np.where(rng.random(B) < 0.1, rng.integers(800, 3000, size=B), rng.integers(0, 300, size=B))
+    call = Q4Call(fd, kv=kv, k=rng.integers(1, 4, size=B), m=rng.integers(0, 3, size=B), hq=2 * hkv, hkv=hkv, dim=dim, seed=B)
+    assert items_of(call, hkv) >= ROUND and B <= 256
+    out, lse = call.upload().run()
+    call.check(out, lse)
+    assert_rows_hold(call, out)
+    assert int(call.status.item()) == 0
+
+
+@pytest.mark.parametrize("blocks", [None, 4])
+def test_more_items_than_run_at_once_of_many_rows(fd, blocks):
+    """Eight sequences of up to 272 new rows: whole items beside tails of 32, 64 and 128 tile rows, in several rounds."""
+    n = np.array([272, 272, 265, 257, 200, 272, 259, 130])
+    k = np.array([16, 16, 9, 1, 200, 12, 3, 130])
+    nb = None if blocks is None else np.where((n - k) % blocks == 0, blocks, 1)
+    call = Q4Call(fd, kv=[700, 3, 0, 90, 300, 1200, 31, 64], k=k, m=n - k, hq=32, hkv=8, blocks=nb, seed=51)
+    assert items_of(call, 8) >= ROUND
+    out, lse = call.upload().run()
+    call.check(out, lse)
+    assert_rows_hold(call, out)
+    assert int(call.status.item()) == 0
+
+
+@pytest.mark.parametrize("B,longest,alone", [(5, 4000, True), (8, 2500, True), (8, 14000, False), (24, 2000, False), (70, 900, False)])
+def test_whole_items_and_tails_in_one_round(fd, B, longest, alone):
+    """Fewer items than work-groups that run at once, with more of the shortest pieces than those: how far whole items of 128 tile rows and tails are cut is
+    found by bisection.  alone: one piece a compute unit; else two."""
+    rng = np.random.default_rng(B)
+    kv, n = rng.integers(longest // 2, longest + 1, size=B), rng.choice([100, 97, 33, 70, 64], size=B)
+    k = np.minimum(n, rng.integers(1, 30, size=B))
+    call = Q4Call(fd, kv=kv, k=k, m=n - k, hq=8, hkv=2, seed=B)
+    if B == 70:                                                   # (more than a wave's lanes: lengths through LDS)
+        n = rng.choice([33, 40], size=B)
+        call = Q4Call(fd, kv=kv, k=n, m=0 * n, hq=8, hkv=2, seed=B)
+    items, blocks = items_of(call, 2), -(-call.kv // 32) + 4 + 3 * -(-call.n // 32)
+    tail = call.n * 4 % 128
+    weight = call.n * 4 // 128 * 6 + np.select([tail == 0, tail <= 32, tail <= 64], [0, 2, 3], 6)           # how long a block takes, in halves
+    assert (items <= ROUND // 4 and 2 * int((blocks * weight).sum()) <= ROUND // 2 * 192) == alone
+    shortest = 2 * int((-(-call.n * 4 // 128) * (blocks // 8 + 1)).sum())
+    assert items < ROUND and shortest > (ROUND // 2 if alone else ROUND)
+    out, lse = call.upload().run()
+    call.check(out, lse)
+    assert_rows_hold(call, out)
+    assert int(call.status.item()) == 0
