@@ -378,7 +378,7 @@ FD_API fd_status fd_step_tables(const fd_table_args *args, void *hip_stream);
  * for the pairs i < rotary_dim / 2: a = i, b = i + rotary_dim / 2, or with interleaved != 0 a = 2 i, b = 2 i + 1; elements from
  * rotary_dim on are not rotated.  Everything is computed in fp32 (the angle's turns in fp64) and rounded once.
  * Inputs are [total_rows][heads][D] with strides in elements between rows and heads (multiples of 4; the last dimension is
- * contiguous), so the parts of one fused projection can be given as they are.  Outputs are dense.  q_out may be q and
+ * contiguous), so the parts of one fused projection can be given as they are.  Tensors and weights are 16-byte aligned.  Outputs are dense.  q_out may be q and
  * k_out may be k where the input is dense; else no output may overlap an input.  v and v_out, if given, are
  * num_kv_heads heads that are copied as they are.
  */
@@ -436,6 +436,8 @@ typedef struct fd_q4_cache {
  * ignored (there is nothing to plan), FD_ATTN_FORCE_GENERIC refused.  kv_chunk > 0 (a multiple of 64) is about the number of keys
  * of one sequence and head that a work-group takes (own rows count more, and pieces of an item are equal).  Workspace: fd_verify_draft_attn_q4_workspace(args) bytes, device,
  * 256-byte aligned; nothing in it has to start at zero or survive a call, and calls that may overlap need one each.
+ * Every work-group finds its piece in the lengths of all sequences, 64 at a time, so that the search grows with the square of the batch: 8 KV heads,
+ * 64 keys and one row each, 256 sequences 60 us a call, 1024 370 us, 4096 4.5 ms.  Larger batches are cheaper in calls of some hundred sequences each.
  * Asynchronous on hip_stream.  Errors: FD_ERR_INVALID_ARG, FD_ERR_UNSUPPORTED, FD_ERR_WORKSPACE_TOO_SMALL, FD_ERR_HIP.
  */
 FD_API fd_status fd_verify_draft_attn_q4(const fd_attn_args *args, const fd_q4_cache *cache, void *hip_stream);
@@ -457,6 +459,8 @@ FD_API fd_status fd_append_kv_q4(const fd_attn_args *args, const fd_q4_cache *ca
  *   out_indptr  device int32 [B+1], not decreasing, up to total_rows (else FD_DEV_ROWS_RANGE)
  *   total_rows  rows of k_out and v_out: total_rows + 128 * min(B, total_rows) < 2^30 (one launch)
  *   status      device uint32[1] or NULL
+ * Page lists end at page_indices_len, also where that is 0.  Every work-group looks for its tokens in the offsets of all sequences, 64 at a time (8 heads and 16 rows
+ * each: 256 sequences 14 us a call, 1024 73 us, 4096 0.9 ms).
  * Asynchronous on hip_stream.  Errors: FD_ERR_INVALID_ARG, FD_ERR_UNSUPPORTED, FD_ERR_HIP.
  */
 FD_API fd_status fd_read_kv_q4(const fd_q4_cache *cache, int32_t batch, int32_t num_kv_heads, int32_t head_dim, int32_t page_size,

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from oracle import kv4
-from tests.q4_harness import device_cache, i32
+from tests.q4_harness import Q4Call, assert_cache_is, device_cache, i32
 
 pytestmark = pytest.mark.gpu
 
@@ -32,3 +32,27 @@ def test_offsets_that_contradict_each_other_are_reported(fd, offsets, whole):
         wk, wv = kv4.read(cache, [0, 1, 2, 3], [2, 0, 3], [0, 0, 0], [0] * (i + 1) + [b - a] * (3 - i))
         at = [r - a for r in rows]
         assert np.array_equal(k[rows].double().cpu().numpy(), wk[at]) and np.array_equal(v[rows].double().cpu().numpy(), wv[at])
+
+
+def test_a_thousand_sequences(fd):
+    """Attention, commit and read-back of a batch that takes many rounds of 64 sequences, some without rows or without a prefix."""
+    B = 1000
+    rng = np.random.default_rng(8)
+    kv, k = rng.integers(0, 40, size=B), rng.integers(0, 3, size=B)
+    kv[rng.random(B) < 0.2] = 0
+    call = Q4Call(fd, kv=kv, k=k, m=rng.integers(0, 2, size=B), hq=4, hkv=2, dim=64, room=2, seed=8).upload()
+    call.check(*call.run())
+    accept = np.maximum(k - 1, 0)
+    lens = torch.zeros(B, dtype=torch.int32, device="cuda")
+    fd.fd_append_kv_q4(call.args, call.dev, i32(accept), lens)
+    wide = lambda bits: (np.asarray(bits).astype(np.uint32) << 16).view(np.float32).astype(np.float64)  # noqa: E731
+    want, after = kv4.append(call.cache, wide(call.k_new), wide(call.v_new), call.page_indptr, call.page_indices, call.kv, call.row_indptr, call.k, accept)
+    assert np.array_equal(lens.cpu().numpy(), after)
+    assert_cache_is(call.dev, want)
+    start = np.minimum(rng.integers(0, 12, size=B), after)
+    offsets = np.r_[0, np.cumsum(after - start)]
+    out = [torch.full((int(offsets[-1]) + 1, 2, 64), -3.0, device="cuda") for _ in range(2)]
+    fd.fd_read_kv_q4(call.dev, call.d["page_indptr"], call.d["page_indices"], i32(start), i32(offsets), *out, status=call.status)
+    for x, w in zip(out, kv4.read(want, call.page_indptr, call.page_indices, start, offsets)):
+        assert np.array_equal(x[:-1].double().cpu().numpy(), w) and (x[-1] == -3).all()
+    assert int(call.status.item()) == 0
