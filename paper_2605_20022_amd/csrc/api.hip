@@ -528,11 +528,17 @@ fd_status fd_qk_norm_rope(const fd_rope_args* a, void* hip_stream) {
   return FD_OK;
 }
 
-static fd_status check_q4_cache(const fd_q4_cache* c, int head_dim, int page_size, int num_kv_heads, int num_pages) {
-  if (!c) return fail(FD_ERR_INVALID_ARG, "cache is NULL");
+static fd_status check_q4_sizes(int head_dim, int page_size, int num_kv_heads) {
   if (head_dim != 128 && head_dim != 64) return fail(FD_ERR_UNSUPPORTED, "a cache in 4 bits has head_dim 128 or 64, not %d", head_dim);
   if (page_size <= 0 || page_size % 16) return fail(page_size <= 0 ? FD_ERR_INVALID_ARG : FD_ERR_UNSUPPORTED, "page_size %d of a cache in 4 bits must be a positive multiple of 16", page_size);
   if (num_kv_heads <= 0 || num_kv_heads > 65535) return fail(FD_ERR_INVALID_ARG, "num_kv_heads %d", num_kv_heads);
+  return FD_OK;
+}
+
+static fd_status check_q4_cache(const fd_q4_cache* c, int head_dim, int page_size, int num_kv_heads, int num_pages) {
+  if (!c) return fail(FD_ERR_INVALID_ARG, "cache is NULL");
+  fd_status st = check_q4_sizes(head_dim, page_size, num_kv_heads);
+  if (st != FD_OK) return st;
   if (c->stride_page < 0 || c->stride_head < 0 || c->stride_page >= (1ll << 31) || c->stride_head >= (1ll << 31))
     return fail(FD_ERR_INVALID_ARG, "cache strides must be in [0, 2^31) blocks");
   // The attention numbers slots in 32 bits, over all blocks between the first and the last that is used, gaps included (2^32 of them without
@@ -568,7 +574,8 @@ static fd_status plan_attn_q4(const fd_attn_args* a, size_t* need) {
   if (st != FD_OK) return st;
   if (a->num_q_heads <= 0 || a->num_kv_heads <= 0 || a->num_q_heads % a->num_kv_heads)
     return fail(FD_ERR_INVALID_ARG, "num_q_heads %d must be a positive multiple of num_kv_heads %d", a->num_q_heads, a->num_kv_heads);
-  if (a->head_dim != 128 && a->head_dim != 64) return fail(FD_ERR_UNSUPPORTED, "a cache in 4 bits has head_dim 128 or 64, not %d", a->head_dim);
+  st = check_q4_sizes(a->head_dim, a->page_size, a->num_kv_heads);
+  if (st != FD_OK) return st;
   if (a->flags & FD_ATTN_FORCE_GENERIC) return fail(FD_ERR_UNSUPPORTED, "there is no full-precision kernel over a cache in 4 bits");
   if (!(a->sm_scale >= 0.f) || isinf(a->sm_scale)) return fail(FD_ERR_INVALID_ARG, "sm_scale must be finite and >= 0");
   if (a->kv_chunk < 0 || a->kv_chunk % 64) return fail(FD_ERR_INVALID_ARG, "kv_chunk %d must be a non-negative multiple of 64", a->kv_chunk);

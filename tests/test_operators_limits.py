@@ -74,3 +74,14 @@ def test_slots_are_numbered_in_32_bits(page_size, pages, heads, stride_page, str
     assert calls == ([1, 1, 1] if fits else [2, 2, 2])            # (what fits: the missing pointer has its turn)
     if not fits:
         assert b"2^32" in fd.load().fd_last_error()
+
+
+def test_no_workspace_for_a_call_that_is_refused():
+    """Heads and page sizes that the attention refuses need no workspace, 0 says so; the products of the largest sizes do not wrap to a small one."""
+    need = lambda **kw: fd.load().fd_verify_draft_attn_q4_workspace(C.byref(_attn(**kw)))  # noqa: E731
+    most = (1 << 31) - 1
+    for kw in (dict(num_kv_heads=65536, num_q_heads=65536), dict(num_kv_heads=most, num_q_heads=most, batch=65535, max_new_rows=1 << 24, total_rows=most),
+               dict(num_kv_heads=65535, num_q_heads=65535, batch=65535, max_new_rows=1 << 24, total_rows=most, max_kv_len=1 << 30, kv_chunk=64),
+               dict(page_size=24), dict(page_size=0), dict(page_size=-16)):
+        assert need(**kw) == 0, kw
+    assert need(num_kv_heads=65535, num_q_heads=65535, batch=1, total_rows=1, max_new_rows=1) > 0
