@@ -18,9 +18,9 @@
 // are two runs of eight keys, as the second product wants them.
 //
 // What bounds it: a block of 32 rows and 32 keys takes a SIMD 0.24 us of matrix instructions and 0.30 us of others, of which little runs side by side
-// (0.5 us measured, two waves): 2 sequences of 2048 to 8192 keys, 272 rows and 32 query heads 64.0 us a call, 711 TFLOP/s.  With few rows HBM, for which
-// the same arithmetic leaves little time: 128 sequences of 1024 to 8192 keys, up to 16 rows 173 us, 3.9 TB/s.  One short sequence is latency
-// (15.2 us): lengths, pages, codes, merge, second launch.
+// (0.5 us measured, two waves): 2 sequences of 2048 to 8192 keys, 272 rows and 32 query heads 68 us a call, 668 TFLOP/s.  With few rows HBM, for which
+// the same arithmetic leaves little time: 128 sequences of 1024 to 8192 keys, up to 16 rows 174 us, 3.8 TB/s.  One short sequence is latency
+// (15.5 us): lengths, pages, codes, merge, second launch.
 #include "kv_q4.h"
 #include "q4_shape.h"
 
@@ -93,12 +93,12 @@ __device__ __forceinline__ int wave_max(int v) {         // of values >= 0
 // a time: the lengths are one latency of memory, the rest LDS of its own and lane shifts, and no wave waits for another.  false: none.
 //
 // How many pieces: with fewer than Q4_SLOTS items as many as run at once, found by bisection, so that one round does it (16 sequences of 512 to
-// 4096 keys 26.6 us a call, in rounds 32.9; 2 of 272 rows 64.6, 78.9): a piece's start and
+// 4096 keys 27.3 us a call, in rounds 35.4; 2 of 272 rows 67.7, 84.2): a piece's start and
 // end cost about as much as twelve blocks (find, pages, first codes, merge), and a second round would wait for the first.  Else Q4_PIECES and
 // the items themselves, dealt out as work-groups become free, the sequences with the longest pieces first: one that began last would be waited for
-// (128 sequences of 1024 to 8192 keys: 173 us, in the order of the batch 203; 768 pieces and items 182).
+// (128 sequences of 1024 to 8192 keys: 173 us, in the order of the batch 201; 768 pieces and items 182).
 //
-// FEW (up to 64 sequences): lengths stay in registers (16 sequences 26.6 us, by the general variant 28.8, whose code is longer and cold).
+// FEW (up to 64 sequences): lengths stay in registers (16 sequences 27.3 us, by the general variant 30.2, whose code is longer and cold).
 template <bool FEW>
 __device__ __forceinline__ bool q4_find(const AttnParams& p, const Q4Sched& sc, int w, int4* kept, Q4Piece& out) {
   const int lane = threadIdx.x & 63;
@@ -380,7 +380,7 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
   b += (slot - (b - first)) & (KS - 1);
   RowWindow win = row_window(nr, s);
   if (!row_on) win = RowWindow{0, 0, 0};
-  // a block that none of the wave's rows sees is passed over (2 sequences of 16 verify rows and 16 mask blocks of 16, where a row sees one: 64.6 us, else 74.8)
+  // a block that none of the wave's rows sees is passed over (2 sequences of 16 verify rows and 16 mask blocks of 16, where a row sees one: 67.7 us, else 76.8)
   auto seen_from = [&](int b) FD_INLINE {
     while (b < last) {
       const int t0 = 32 * (b - cached);
@@ -632,7 +632,7 @@ __global__ __launch_bounds__(Q4_BLOCK, 2) void attn_q4_kernel(AttnParams p, Q4Ca
 
 // Merge of the partials of split items, by rows: a row is taken by TPR = DH / 8 lanes, eight channels each.  AT_ONCE pieces at a time, lane j of them
 // knows the maximum and sum of piece j; their values are requested with those, so that a batch is one latency.  Where an item may have many pieces,
-// 2^group_shift such groups of lanes share a row's and meet in LDS (1 sequence of 32 768 keys: 24.4 us a call, with one group 33.1).
+// 2^group_shift such groups of lanes share a row's and meet in LDS (1 sequence of 32 768 keys: 25.6 us a call, with one group 33.2).
 template <int DH>
 __global__ __launch_bounds__(256) void attn_q4_combine_kernel(AttnParams p, Q4Sched sc, int group_shift) {
   constexpr int TPR = DH / 8, SETS = 256 / TPR, AT_ONCE = 8;
@@ -728,8 +728,8 @@ hipError_t run_attn_q4(const AttnParams& p, const Q4Cache& c, void* workspace, i
   char* ws = reinterpret_cast<char*>(workspace);
   const Q4Sched sc = {z.fixed, z.fixed > 0 ? 1.f / (float)z.fixed : 0.f, z.unit_shift, z.rt_max, (int)z.partials, reinterpret_cast<float*>(ws), reinterpret_cast<float*>(ws + z.off_ml), reinterpret_cast<int2*>(ws + z.off_entries)};
   if (z.wgs == 0) return hipSuccess;
-  // Pieces of an item, if the call's items are about equal: four of them to a group of lanes, so that twice as many are one batch (eight: the same within
-  // 1%; two: 2 sequences of 272 rows 64.6 -> 66.4 us).
+  // Pieces of an item, if the call's items are about equal: four of them to a group of lanes, so that twice as many are one batch (eight: 2 sequences of 272
+  // rows 67.7 -> 67.2 us, 1 of 32 768 keys 25.6 -> 25.8; two: 2 of 272 rows 70.3).
   const int sets = 256 / (p.D / 8), most_rows = (int)((long long)p.max_new_rows * p.G < Q4_ROWS ? p.max_new_rows * p.G : Q4_ROWS);
   const long long pieces = z.fixed > 0 ? z.max_pieces : z.max_pieces < Q4_SLOTS / z.items ? z.max_pieces : Q4_SLOTS / z.items;
   int group_shift = 0;

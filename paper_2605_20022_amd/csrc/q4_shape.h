@@ -7,15 +7,15 @@ namespace fd {
 constexpr int Q4_TK = 32;                 // keys of a block
 constexpr int Q4_ROWS = 128;              // tile rows of an item
 constexpr int Q4_SLOTS = 512;             // work-groups that run at once: two a compute unit
-// Units a compute unit up to which it takes one piece (one sequence of 32 768 keys, 64 rows, 99 units: 24.4 us a call, in twice as many pieces 27.4;
-// 4 of 8192 to 16 384, 146: 30.4 and 32.1; one of 8192, 272 rows, 420: 56.8 and 54.5).
+// Units a compute unit up to which it takes one piece (one sequence of 32 768 keys, 64 rows, 99 units: 25.6 us a call, in twice as many pieces 29.1;
+// 4 of 8192 to 16 384, 146: 31.3 and 33.1; one of 8192, 272 rows, 420: 60.8 and 58.6).
 constexpr int Q4_ALONE = 192;
 constexpr int Q4_PIECES = 512;            // pieces aimed at where there are Q4_SLOTS items or more
 constexpr int Q4_CLASSES = 4;             // lengths of pieces that are told apart
-// A block of own rows takes as long as Q4_OWN of cached ones, the first Q4_OWN_START more (1 sequence of 16 new rows 15.1 us a call, 2 of 272 in 17
-// blocks 64.5; counted as cached ones 16.6 and 66.4, with 6 more 15.2 and 66.0).
+// A block of own rows takes as long as Q4_OWN of cached ones, the first Q4_OWN_START more (1 sequence of 16 new rows 15.4 us a call, 2 of 272 in 17
+// blocks 67.7; counted as cached ones 17.0 and 70.0, the first 6 more 16.0 and 70.0).
 constexpr int Q4_OWN = 3, Q4_OWN_START = 4;
-constexpr int Q4_MIN_PIECE = 8;           // blocks of a piece, at least, but for the last of a short item (1 sequence of 1024 keys 14.1 us; 6: 14.8, 12: 14.6)
+constexpr int Q4_MIN_PIECE = 8;           // blocks of a piece, at least, but for the last of a short item (1 sequence of 1024 keys 14.2 us; 6: 15.0, 12: 14.5)
 constexpr int Q4_KEPT = 4;                // rounds of 64 sequences whose lengths a wave keeps in LDS
 
 // Items of the largest sequence, partial slots and work-groups that there can be, and the workspace.
