@@ -377,7 +377,7 @@ FD_API fd_status fd_step_tables(const fd_table_args *args, void *hip_stream);
  *     (y_a, y_b) -> (y_a cos t - y_b sin t, y_b cos t + y_a sin t),  t = positions[row] * inv_freq[i]
  * for the pairs i < rotary_dim / 2: a = i, b = i + rotary_dim / 2, or with interleaved != 0 a = 2 i, b = 2 i + 1; elements from
  * rotary_dim on are not rotated.  Everything is computed in fp32 (the angle's turns in fp64) and rounded once.
- * Inputs are [total_rows][heads][D] with strides in elements between rows and heads (multiples of 4; the last dimension is
+ * Inputs are [total_rows][heads][D] with strides in elements between rows and heads (multiples of 4, or anything where there is one; the last dimension is
  * contiguous), so the parts of one fused projection can be given as they are.  Tensors and weights are 16-byte aligned.  Outputs are dense.  q_out may be q and
  * k_out may be k where the input is dense; else no output may overlap an input.  v and v_out, if given, are
  * num_kv_heads heads that are copied as they are.

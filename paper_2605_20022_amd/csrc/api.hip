@@ -517,13 +517,17 @@ fd_status fd_qk_norm_rope(const fd_rope_args* a, void* hip_stream) {
     return fail(FD_ERR_INVALID_ARG, "a required device pointer is NULL");
   if (a->num_kv_heads > 0 && !a->v != !a->v_out) return fail(FD_ERR_INVALID_ARG, "v and v_out are given together or not at all");
   if (a->rotary_dim > 0 && (!a->inv_freq || !a->positions)) return fail(FD_ERR_INVALID_ARG, "rotary_dim > 0 needs inv_freq and positions");
-  const int64_t strides[] = {a->q_stride_row, a->q_stride_head, a->k_stride_row, a->k_stride_head, a->v ? a->v_stride_row : 0, a->v ? a->v_stride_head : 0};
+  fd_rope_args r = *a;
+  if (r.total_rows == 1) r.q_stride_row = r.k_stride_row = r.v_stride_row = 0;          // a stride that leads nowhere may be anything
+  if (r.num_q_heads <= 1) r.q_stride_head = 0;
+  if (r.num_kv_heads <= 1) r.k_stride_head = r.v_stride_head = 0;
+  const int64_t strides[] = {r.q_stride_row, r.q_stride_head, r.k_stride_row, r.k_stride_head, r.v ? r.v_stride_row : 0, r.v ? r.v_stride_head : 0};
   for (int64_t s : strides)
     if (s < 0 || s % 4) return fail(FD_ERR_INVALID_ARG, "strides must be non-negative multiples of 4 elements (%lld)", (long long)s);
   const void* ptrs[] = {a->q, a->k, a->v, a->q_out, a->k_out, a->v_out, a->q_weight, a->k_weight};
   for (const void* p : ptrs)
     if (!aligned16(p)) return fail(FD_ERR_INVALID_ARG, "q, k, v, the weights and the outputs must be 16-byte aligned");
-  hipError_t e = fd::run_qk_norm_rope(*a, reinterpret_cast<hipStream_t>(hip_stream));
+  hipError_t e = fd::run_qk_norm_rope(r, reinterpret_cast<hipStream_t>(hip_stream));
   if (e != hipSuccess) return fail(FD_ERR_HIP, "norm and rotation launch: %s", hipGetErrorString(e));
   return FD_OK;
 }

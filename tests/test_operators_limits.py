@@ -6,7 +6,7 @@ import subprocess
 import pytest
 
 from paper_2605_20022_amd import flexdraft as fd
-from tests.test_operators_host import P, ROOT, _attn, _cache, _refused, _tables
+from tests.test_operators_host import P, ROOT, _attn, _cache, _refused, _rope, _tables
 
 
 @pytest.mark.parametrize("entries", ["page_indices_len", "free_pages_len"])
@@ -85,3 +85,12 @@ def test_no_workspace_for_a_call_that_is_refused():
                dict(page_size=24), dict(page_size=0), dict(page_size=-16)):
         assert need(**kw) == 0, kw
     assert need(num_kv_heads=65535, num_q_heads=65535, batch=1, total_rows=1, max_new_rows=1) > 0
+
+
+def test_strides_of_dimensions_of_one_do_not_matter():
+    """Between rows where there is one row, and between heads where there is one: any number.  (The next check has its turn: the call is not made.)"""
+    for kw in (dict(total_rows=1, q_stride_row=1, k_stride_row=-3), dict(num_q_heads=1, q_stride_head=65), dict(num_kv_heads=1, k_stride_head=1),
+               dict(num_kv_heads=1, total_rows=1, v=P, v_out=P, v_stride_row=7, v_stride_head=9)):
+        _refused(_rope(**dict(kw, q=P + 8)), 1, "aligned")
+    for kw in (dict(total_rows=2, q_stride_row=1), dict(num_q_heads=2, q_stride_head=65), dict(num_kv_heads=2, k_stride_head=1)):
+        _refused(_rope(**kw), 1, "strides")
