@@ -1,6 +1,7 @@
 """How the attention over a 4-bit cache cuts items into pieces, and what its pieces leave of a row: GPU parity against the fp64 oracle."""
 import numpy as np
 import pytest
+import torch
 
 from oracle import attention as oa
 from oracle import kv4
@@ -112,3 +113,51 @@ def test_whole_items_and_tails_in_one_round(fd, B, longest, alone):
     call.check(out, lse)
     assert_rows_hold(call, out)
     assert int(call.status.item()) == 0
+
+
+# ---- calls beside each other ------------------------------------------------------------------
+def _bits(call):
+    torch.cuda.synchronize()
+    return call.out.view(torch.int16).clone(), call.lse.view(torch.int32).clone()
+
+
+def test_graphs_that_share_a_workspace(fd):
+    """Two captured calls of different shape on one workspace, replayed in turn with eager work in between: nothing in it has to survive, or to be what it was."""
+    calls = [Q4Call(fd, kv=[900, 33], k=[4, 2], m=[4, 0], seed=61).upload(), Q4Call(fd, kv=[20, 1500], k=[1, 2], m=[4, 9], seed=62).upload()]
+    shared = fd.alloc_workspace(max(c.workspace.numel() for c in calls))
+    graphs, want = [], []
+    for c in calls:
+        c.args.workspace, c.args.workspace_bytes = shared.data_ptr(), shared.numel()
+        c.check(*c.run())
+        want.append(_bits(c))
+    for c in calls:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            fd.fd_verify_draft_attn_q4(c.args, c.dev)
+    for turn in (0, 1, 0, 0, 1, 1, 0):
+        c = calls[turn]
+        c.out.fill_(-7)
+        shared.random_(0, 255)
+        graphs[turn].replay()
+        for got, w in zip(_bits(c), want[turn]):
+            assert torch.equal(got, w)
+
+
+def test_pages_that_several_sequences_share(fd):
+    """A common prefix: three lists of the same pages."""
+    call = Q4Call(fd, kv=[64, 64, 64], k=[2, 3, 1], m=[1, 0, 4], seed=63)
+    call.page_indices[4:8] = call.page_indices[8:12] = call.page_indices[:4]
+    call.upload()
+    out, lse = call.run()
+    call.check(out, lse)
+    assert_rows_hold(call, out)
+
+
+@pytest.mark.parametrize("B", [3, 70, 300])
+def test_sequences_without_rows(fd, B):
+    """A batch none of whose sequences brings a row: nothing is written, and nothing is amiss."""
+    call = Q4Call(fd, kv=[50] * B, k=[1] + [0] * (B - 1), m=[0] * B, spare_rows=4, seed=64).upload()
+    call.d["row_indptr"].zero_()
+    call.d["verify_len"].zero_()
+    out, lse = call.run()
+    assert (out == -7).all() and (lse == -7).all() and int(call.status.item()) == 0
